@@ -456,6 +456,115 @@ int d3tom_stack_step_batch(const void* x, int B, const int32_t* N /* host */, in
                            void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * A key/value cache in pages (Section 4.4, "Compatibility with KV-Cache": the rows of prompt and visual tokens are kept
+ * between steps).  Slot j of sample b is row j % page_size of page page_table[b * table_stride + j / page_size].  Samples may
+ * share pages that are only read.
+ *
+ *   k_pages, v_pages  [num_pages, page_size, Hkv, dh] dt
+ *   page_table        int32[B, table_stride]; entries behind a sample's last page are never read
+ *   kv_len            int32[B]  live slots of each sample.  The caller advances it BEFORE the rows are written: a call that appends
+ *                     or attends from n new rows has them in slots kv_len - n .. kv_len - 1, and can be repeated.
+ *   page_size         a power of two, 16 .. 4096          dh  a multiple of 8 (bf16) or 4 (f32), at most 256
+ *   B                 at most 65535
+ * A page that is not among the num_pages is clamped where it is read and skipped where it would be written; a length outside
+ * 0 .. max_len is clamped.  The struct itself is HOST memory and is read during the call only.
+ * ---------------------------------------------------------------------------------------- */
+typedef struct {
+    void* k_pages;
+    void* v_pages;
+    const int32_t* page_table;
+    const int32_t* kv_len;
+    int32_t num_pages, page_size, table_stride, B, Hkv, dh, dt;
+} d3tom_paged_cache;
+
+/* Rotary positions with several axes (time, height, width of a video's patches; row and column of an image's).  Channel c < dh/2
+ * of every head is paired with channel c + dh/2 as in d3tom_rope.  The pairs are cut into `axes` sections, pairs[a] consecutive
+ * ones for axis a; a pair of axis a turns by pos[row, a] times its frequency, pairs behind the last section are left as they are.
+ *   pos       int32[rows, axes] (device)     axes 1 .. D3TOM_MAX_AXES     pairs[a] >= 1, their sum at most dh/2
+ *   ladder    D3TOM_AXES_SHARED  pair c has theta^(-2c/dh), whatever its axis (one axis of dh/2 pairs: d3tom_rope)
+ *             D3TOM_AXES_OWN     pair u of axis a has theta^(-u/pairs[a]): every axis has all frequencies
+ *   theta     finite and > 1
+ * HOST memory, read during the call only. */
+#define D3TOM_MAX_AXES 4
+typedef enum { D3TOM_AXES_SHARED = 0, D3TOM_AXES_OWN = 1 } d3tom_axes_ladder;
+typedef struct {
+    const int32_t* pos;
+    int32_t axes, pairs[D3TOM_MAX_AXES], ladder;
+    float theta;
+} d3tom_axes;
+
+/* d3tom_rope_axes: q_out, k_out = q, k turned by the rows' positions.  f32 or bf16, float32 arithmetic on angles that are reduced in
+ * double precision, one rounding.
+ *   q, k          [rows, H, dh], [rows, Hkv, dh] dt, rows q_stride / k_stride ELEMENTS apart (a multiple of 16 bytes; columns of a stacked
+ *                 projection); one of the two may be NULL
+ *   q_out, k_out  [rows, H, dh], [rows, Hkv, dh] dt contiguous; may be q / k themselves where those are contiguous
+ *   dh            a multiple of 16 (bf16) or 8 (f32), at most 256 */
+int d3tom_rope_axes(const void* q, int64_t q_stride, const void* k, int64_t k_stride, int dt, int rows, int H, int Hkv, int dh,
+                    const d3tom_axes* axes /* host */, void* q_out, void* k_out, void* stream);
+
+/* d3tom_cache_append: new rows into the pages, row i of sample b's n new ones into slot kv_len[b] - n + i; rows whose slot is
+ * negative are not written.  With axes, keys are turned on the way (and queries beside them, into q_out); v is copied.
+ *   k, v         [rows, Hkv, dh] dt, k_stride / v_stride elements between rows (a multiple of 16 bytes)
+ *   new_off      int32[B + 1]  first new row of each sample; rows = new_off[B] (host-known), max_new the longest run
+ *   axes         host or NULL: keys as they are (then q has to be NULL)
+ *   q, q_out     [rows, H, dh] (q_stride apart) and [rows, H, dh] contiguous, or both NULL; q_out may be q where that is contiguous
+ *   tokens       int32[rows] or NULL; with slot_token int32[B, slot_stride]: the slots' entries become the rows' (a token's number in
+ *                its sample, which d3tom_cache_evict reads)
+ *   slot_weight  float[B, slot_stride] or NULL: the slots' entries become 0
+ * With axes dh is a multiple of 16 (bf16) or 8 (f32). */
+int d3tom_cache_append(const d3tom_paged_cache* cache /* host */, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                       const int32_t* new_off, int rows, int max_new, const d3tom_axes* axes /* host */,
+                       const void* q, int64_t q_stride, int H, void* q_out,
+                       const int32_t* tokens, int32_t* slot_token, float* slot_weight, int slot_stride, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * d3tom_attend_cache — attention of each sample's newest rows over its cache (the step of a model that keeps one: a token, a few
+ * drafted ones, or the block of response positions that is being denoised).  Per row and head h, keys and values of head
+ * h / (H / Hkv):  o = softmax(scale * q k^T) v over the sample's live slots, or, causal, over those up to the row's own slot
+ * (row i of n: slot kv_len[b] - n + i).  A row that sees no slot gets zeros and lse -infinity.  What lies behind a sample's last
+ * slot is never used, NaN included.
+ *
+ *   q          [rows, H, dh] dt, q_stride elements between rows (a multiple of 16 bytes); H a multiple of Hkv
+ *   q_off      int32[B + 1]  first row of each sample; rows = q_off[B] (host-known), max_q the longest run, max_len the longest cache
+ *   o          [rows, H, dh] dt contiguous, out           lse  float[rows, H] out or NULL: log sum exp of the row's logits
+ *   weight_out float[B, weight_stride] out or NULL: for every live slot weight_in plus the probabilities that the sample's rows give
+ *              it, added over rows and averaged over heads (the importance map with all rows as deciders); other slots are left as they are
+ *   weight_in  float[B, weight_stride] or NULL (zeros); may be weight_out
+ * bf16: the probabilities enter the product with v as bf16, relative to the running maximum of their row, all sums are float32.
+ * Long caches are cut into runs of slots whose results are joined; how goes by the host-known sizes only, so that a call has
+ * the same bits whatever the cache's unused slots hold.  No size is a limit but: rows * H and B * H at most 2^31 - 1 workgroups.
+ * Workspace: d3tom_attend_cache_workspace_bytes (weighed: whether weight_out is given; 0 for arguments that the call refuses).
+ * ---------------------------------------------------------------------------------------- */
+size_t d3tom_attend_cache_workspace_bytes(const d3tom_paged_cache* cache /* host */, int rows, int max_q, int max_len, int H, int weighed);
+int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_paged_cache* cache /* host */, const int32_t* q_off, int rows, int max_q,
+                       int max_len, int H, float scale, int causal, void* o, float* lse, const float* weight_in, float* weight_out,
+                       int weight_stride, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * d3tom_cache_evict — a cache shortened by the attention weight that its slots have got.  Of sample b's n = kv_len[b] slots the
+ * k = min(keep[b], n) first in this order stay: protected ones in front of all others; then the larger weight; then the lower slot
+ * (protected ones among themselves: the lower slot).  Protected are tokens numbered below `first` and the `recent` last numbers, those above
+ * (the largest number of a live slot) - recent.  Slots below k that do not stay are filled, in ascending order, with the rows of
+ * the staying slots from k on, in ascending order, so that nothing else moves: attention does not ask for the order of its keys, and rows are
+ * turned by their positions before they are written.  The pages behind slot k are free.
+ *
+ *   cache      the rows are moved in place (all Hkv heads of k_pages and v_pages); pages of different samples must not overlap
+ *   max_len    host-known longest cache, at most D3TOM_MAX_EVICT_LEN
+ *   keep       int32[B], below 0 counts as 0
+ *   weight_in, token_in    float / int32 [B, slot_stride]: weight and token number of every slot; NaN weights are outside the contract
+ *   weight_out, token_out  float / int32 [B, slot_stride] out: the first k entries of a sample, others are left as they are.  May be
+ *              weight_in and token_in themselves; otherwise the call can be repeated
+ *   len_out    int32[B] out: k (may be kv_len)
+ *   src        int32[B, slot_stride] out or NULL: the slot that the row of each of the first k slots comes from
+ * Workspace: d3tom_cache_evict_workspace_bytes.
+ * ---------------------------------------------------------------------------------------- */
+#define D3TOM_MAX_EVICT_LEN 1048576
+size_t d3tom_cache_evict_workspace_bytes(const d3tom_paged_cache* cache /* host */, int max_len);
+int d3tom_cache_evict(const d3tom_paged_cache* cache /* host */, int max_len, const int32_t* keep, int first, int recent,
+                      const float* weight_in, const int32_t* token_in, float* weight_out, int32_t* token_out, int slot_stride,
+                      int32_t* len_out, int32_t* src, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * Per-kernel timing (diagnostics; used by the benchmark for its roofline figures).  While enabled,
  * every kernel launch of the four entry points is bracketed by HIP events on the caller's stream.
  * d3tom_profile_collect waits for the recorded events, adds up milliseconds and launch counts per

@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libd3tom.so")
 NATIVE = os.path.join(HERE, "_native.so")
 SOURCES = ["api.hip", "importance.hip", "topk.hip", "merge.hip", "attend.hip", "deciders.hip", "linear.hip", "block_ops.hip",
-           "stack.hip", "pipeline.hip"]
+           "stack.hip", "pipeline.hip", "rope_axes.hip", "attend_cache.hip", "evict.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",   # no packed-fp32 VALU forms
          "-mllvm", "-amdgpu-kernarg-preload-count=16",                  # first arguments arrive in registers: one load less in front of every kernel

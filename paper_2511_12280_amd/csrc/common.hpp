@@ -288,7 +288,7 @@ inline bool raise_dynamic_lds(K kernel, int bytes) {
 namespace prof {
 enum Kernel {
     IMP_STATS = 0, IMP_SCORES, IMP_FINISH, TOPK_SELECT, MERGE_NORMS, COS_ARGMAX, MERGE_ASSIGN, MERGE_SCATTER, ATTEND,
-    UPDATE_DECIDERS, COS_REDUCE, LINEAR, RMSNORM, ROPE, STACK_META,
+    UPDATE_DECIDERS, COS_REDUCE, LINEAR, RMSNORM, ROPE, STACK_META, CACHE_APPEND, CACHE_ATTEND, CACHE_JOIN, CACHE_WEIGH, EVICT_SELECT, EVICT_MOVE,
     NUM_KERNELS
 };
 extern bool g_enabled;

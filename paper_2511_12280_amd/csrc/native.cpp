@@ -71,6 +71,58 @@ template <> struct Arg<float> {
     }
 };
 
+template <> struct Arg<int64_t> {
+    static int64_t get(PyObject* o) {
+        const long long v = PyLong_AsLongLong(o);
+        if (v == -1 && PyErr_Occurred()) throw PythonError();
+        return v;
+    }
+};
+// None, or a host struct by its buffer (ctypes structures have one)
+template <typename S>
+struct HostStruct {
+    static const S* get(PyObject* o) {
+        if (o == Py_None) return nullptr;
+        Py_buffer view;
+        if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw PythonError();
+        const void* p = view.buf;
+        const bool fits = view.len == (Py_ssize_t)sizeof(S);
+        PyBuffer_Release(&view);                               // the caller holds the object while the call runs
+        if (!fits) { PyErr_SetString(PyExc_ValueError, "a host struct of another size"); throw PythonError(); }
+        return static_cast<const S*>(p);
+    }
+};
+template <> struct Arg<const d3tom_paged_cache*> : HostStruct<d3tom_paged_cache> {};
+template <> struct Arg<const d3tom_axes*> : HostStruct<d3tom_axes> {};
+
+// None, or a tensor [rows, heads, dh] whose rows may lie apart: its address and the elements between two rows
+struct Rows { const void* p; int64_t stride; };
+template <> struct Arg<Rows> {
+    static Rows get(PyObject* o) {
+        if (o == Py_None) return {nullptr, 0};
+        if (!THPVariable_Check(o)) refuse();
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || t.dim() != 3 || (t.size(2) > 1 && t.stride(2) != 1) || (t.size(1) > 1 && t.stride(1) != t.size(2))) {
+            PyErr_SetString(PyExc_ValueError, "rows of heads on the GPU, contiguous inside a row");
+            throw PythonError();
+        }
+        return {t.data_ptr(), t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2)};
+    }
+};
+int rope_axes_rows(Rows q, Rows k, int dt, int rows, int H, int Hkv, int dh, const d3tom_axes* axes, void* q_out, void* k_out, void* stream) {
+    return d3tom_rope_axes(q.p, q.stride, k.p, k.stride, dt, rows, H, Hkv, dh, axes, q_out, k_out, stream);
+}
+int cache_append_rows(const d3tom_paged_cache* cache, Rows k, Rows v, const int32_t* new_off, int rows, int max_new, const d3tom_axes* axes, Rows q,
+                      int H, void* q_out, const int32_t* tokens, int32_t* slot_token, float* slot_weight, int slot_stride, void* stream) {
+    return d3tom_cache_append(cache, k.p, k.stride, v.p, v.stride, new_off, rows, max_new, axes, q.p, q.stride, H, q_out, tokens, slot_token,
+                              slot_weight, slot_stride, stream);
+}
+int attend_cache_rows(Rows q, const d3tom_paged_cache* cache, const int32_t* q_off, int rows, int max_q, int max_len, int H, float scale, int causal,
+                      void* o, float* lse, const float* weight_in, float* weight_out, int weight_stride, void* ws, size_t ws_bytes, void* stream) {
+    return d3tom_attend_cache(q.p, q.stride, cache, q_off, rows, max_q, max_len, H, scale, causal, o, lse, weight_in, weight_out, weight_stride, ws,
+                              ws_bytes, stream);
+}
+
 template <typename T> struct Type { using type = T; };
 
 template <typename... A, size_t... I>
@@ -103,8 +155,9 @@ PyObject* enter(int (*fn)(A...), PyObject* const* args, Py_ssize_t n) {
     }
 }
 
-#define D3TOM_ENTRY(NAME) \
-    PyObject* py_##NAME(PyObject*, PyObject* const* args, Py_ssize_t n) { return enter(&NAME, args, n); }
+#define D3TOM_ENTRY_AS(NAME, FN) \
+    PyObject* py_##NAME(PyObject*, PyObject* const* args, Py_ssize_t n) { return enter(&FN, args, n); }
+#define D3TOM_ENTRY(NAME) D3TOM_ENTRY_AS(NAME, NAME)
 D3TOM_ENTRY(d3tom_importance)
 D3TOM_ENTRY(d3tom_importance_static)
 D3TOM_ENTRY(d3tom_select_topk)
@@ -118,14 +171,20 @@ D3TOM_ENTRY(d3tom_rmsnorm)
 D3TOM_ENTRY(d3tom_rope)
 D3TOM_ENTRY(d3tom_linear)
 D3TOM_ENTRY(d3tom_linear_tile)
+D3TOM_ENTRY_AS(d3tom_rope_axes, rope_axes_rows)
+D3TOM_ENTRY_AS(d3tom_cache_append, cache_append_rows)
+D3TOM_ENTRY_AS(d3tom_attend_cache, attend_cache_rows)
+D3TOM_ENTRY(d3tom_cache_evict)
 #undef D3TOM_ENTRY
+#undef D3TOM_ENTRY_AS
 
 #define D3TOM_METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))py_##NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     D3TOM_METHOD(d3tom_importance), D3TOM_METHOD(d3tom_importance_static), D3TOM_METHOD(d3tom_select_topk), D3TOM_METHOD(d3tom_merge),
     D3TOM_METHOD(d3tom_merge_kv), D3TOM_METHOD(d3tom_merge_layer), D3TOM_METHOD(d3tom_attend), D3TOM_METHOD(d3tom_attend_weighted),
     D3TOM_METHOD(d3tom_update_deciders), D3TOM_METHOD(d3tom_rmsnorm), D3TOM_METHOD(d3tom_rope), D3TOM_METHOD(d3tom_linear),
-    D3TOM_METHOD(d3tom_linear_tile), {nullptr, nullptr, 0, nullptr}};
+    D3TOM_METHOD(d3tom_linear_tile), D3TOM_METHOD(d3tom_rope_axes), D3TOM_METHOD(d3tom_cache_append), D3TOM_METHOD(d3tom_attend_cache),
+    D3TOM_METHOD(d3tom_cache_evict), {nullptr, nullptr, 0, nullptr}};
 #undef D3TOM_METHOD
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
