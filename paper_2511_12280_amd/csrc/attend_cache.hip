@@ -5,6 +5,7 @@
 //   o = sum_s O_s 2^(m_s - m) / sum_s l_s 2^(m_s - m),  m = max_s m_s    (logits in units of log 2).
 // What the slots got (weight_out) is formed from the joined sums behind that: p = 2^(logit - lse).
 #include "cache.hpp"
+#include "direct_load.hpp"
 
 namespace d3tom {
 
@@ -13,12 +14,14 @@ struct AttendCacheArgs {
     const void *q, *k_pages, *v_pages;
     size_t q_stride;
     const int32_t* q_off;
-    int rows, max_q, max_len, H, G, causal;     // G: query heads of a key head
+    int nB, rows, max_q, max_len, H, G, causal; // G: query heads of a key head
     float scale2;                               // scale * log2(e)
     int S, run;                                 // runs of a cache, slots of a run
     void* o;
     float *lse, *lse2;                          // natural logarithm (the caller's), base 2 (for the weights)
     float *part_o, *part_ml;                    // [rows, H, S, dh], [rows, H, S, 2]
+    float* logits;                              // [rows, H, lpad], units of log 2, or none
+    int lpad, tiles;                            // tiles: of 16 rows, of a sample and key head
     const float* weight_in;
     float* weight_out;
     int weight_stride;
@@ -140,26 +143,352 @@ __global__ __launch_bounds__(256) void attend_cache_generic_kernel(AttendCacheAr
     }
 }
 
-// the runs of a row and head joined: one workgroup for each
-template <typename T>
-__global__ __launch_bounds__(256) void attend_cache_join_kernel(AttendCacheArgs a) {
-    const int tid = threadIdx.x, dh = a.cache.dh;
-    const size_t at = blockIdx.x;
-    const float* ml = a.part_ml + at * a.S * 2;
-    float m = -INFINITY;
-    for (int s = 0; s < a.S; ++s) m = fmaxf(m, ml[2 * s]);
-    float z = 0.f, t = 0.f;
-    for (int s = 0; s < a.S; ++s) {
-        if (ml[2 * s] == -INFINITY) continue;
-        const float f = exp2f(ml[2 * s] - m);
-        z += ml[2 * s + 1] * f;
-        if (tid < dh) t += a.part_o[(at * a.S + s) * dh + tid] * f;
+
+// ---- heads of 64 and 128 on the matrix instructions ----------------------------------------------------------------------
+// The rows of a sample that share a key head (G heads of every new row) are the columns of
+//     S^T = K Q^T     A = K (LDS), B = Q^T (registers)
+//     O^T += V^T P^T  A = V^T (LDS; bf16: the transposing read), B = P^T as the accumulators of the first product hold it
+// sixteen of them, MFMA 16x16x32 (bf16) or four 16x16x4 (float32), whose lanes take four neighbouring channels each: the order of a contraction is free.
+// Lane (r, g) = (lane % 16, lane / 16) has column r and, of every 16 keys, keys 4g .. 4g + 3.
+//
+// Bound by memory: a key's row is read for 16 columns at most.  What keeps it busy is bytes in flight, so every wave is on its own, with a ring of two stages (K and V of
+// 8 KB each) that direct loads fill: while one stage is used the other and the next are on their way, and no wave waits for another one before
+// the end, when the four waves of a workgroup join what they have through LDS.
+template <typename T, int DH> struct AcTile {
+    static constexpr int ROWB = DH * (int)sizeof(T), NCHK = ROWB / 16;      // bytes and 16-byte chunks of a row of a head
+    static constexpr int TILE = 8192, KEYS = TILE / ROWB, KB = KEYS / 16;   // of K or V: keys, blocks of 16
+    static constexpr int LD = 8, LDB = LD / KB, RPI = 64 / NCHK;            // direct loads of a tile, of a block; rows of one
+    static constexpr int KS = NCHK / 4, DB = DH / 16;                       // steps of the first product, 16-channel blocks of O^T
+    static constexpr int STAGE = 2 * TILE, WAVE_LDS = 2 * STAGE, PITCH = DH + 4;
+    // what the position of a chunk in a row is turned by, so that the 16 rows of a fragment lie in different banks
+    static __device__ __forceinline__ int k_turn(int row) { return row & (NCHK - 1) & 15; }
+    static __device__ __forceinline__ int v_turn(int row) {
+        if constexpr (sizeof(T) == 4) return ((row >> 2) & 3) * 4;
+        else return NCHK == 16 ? (row & 3) * 4 : ((row >> 1) & 1) * 2;
     }
-    if (tid < dh) Elem<T>::store(static_cast<T*>(a.o) + at * dh + tid, z > 0.f ? t / z : 0.f);
-    if (tid == 0) {
-        const float l2 = z > 0.f ? m + log2f(z) : -INFINITY;
-        if (a.lse) a.lse[at] = l2 * 0.6931471805599453f;
-        if (a.lse2) a.lse2[at] = l2;
+};
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short ac_short4;
+typedef __attribute__((__vector_size__(8 * sizeof(short)))) short ac_short8;
+
+#if defined(__HIP_DEVICE_COMPILE__)
+template <typename T>
+__device__ __forceinline__ f32x4 ac_mma(const uint4& a, const uint4& b, f32x4 c) {
+    if constexpr (sizeof(T) == 2) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    } else {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
+        return c;
+    }
+}
+__device__ __forceinline__ float quad_max(float v) { return quad_combine(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float quad_sum(float v) { return quad_combine(v, [](float a, float b) { return a + b; }); }
+#endif
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    using C = AcTile<T, DH>;
+    constexpr int ROWB = C::ROWB, NCHK = C::NCHK, KEYS = C::KEYS, KB = C::KB, LDB = C::LDB, RPI = C::RPI, KS = C::KS, DB = C::DB;
+    extern __shared__ __attribute__((aligned(16))) char ring[];
+    __shared__ float part_m[4][16], part_l[4][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    // tiles of rows of the same keys run on one XCD, one after the other
+    int id = blockIdx.x;
+    const int xcd = id & 7;
+    id >>= 3;
+    const int tile = id % a.tiles;
+    int unit = (id / a.tiles) * 8 + xcd;
+    const int s = unit % a.S; unit /= a.S;
+    const int kvh = unit % a.cache.Hkv, b = unit / a.cache.Hkv;
+    const int nB = a.nB;
+    if (b >= nB) return;
+    int r0;
+    const int nq = sample_rows(a, b, r0);
+    const int R = nq * a.G, R0 = tile * 16;
+    if (R0 >= R) return;
+    const int n = a.cache.length(b, a.max_len);
+    const int last = min(R0 + 15, R - 1);
+    const int j0 = s * a.run, j1 = min(row_limit(a, n, nq, last / a.G), j0 + a.run);
+    if (j0 >= j1 && s > 0) return;
+    const int x = min(R0 + r, R - 1), xi = x / a.G, xh = kvh * a.G + (x - xi * a.G);          // this lane's column
+    const size_t row = (size_t)(r0 + xi);
+    const int limit = min(row_limit(a, n, nq, xi), j1);
+    const int limit0 = min(row_limit(a, n, nq, R0 / a.G), j1);                                 // slots that all columns see
+
+    // pages of this wave's blocks of 16 slots: lane i has that of block i % KB of its tile i / KB
+    const int ntile = j1 > j0 ? (j1 - j0 + KEYS - 1) / KEYS : 0;
+    const int mine = (ntile - wave + 3) / 4;                                                   // tiles wave, wave + 4, ...
+    const int my_slot = j0 + ((lane / KB) * 4 + wave) * KEYS + (lane % KB) * 16;
+    const uint32_t ids = my_slot < j1 ? a.cache.readable(a.cache.page_of(b, my_slot)) : 0u;
+
+    uint4 qf[KS];
+    {
+        const char* q = static_cast<const char*>(a.q) + (row * a.q_stride + (size_t)xh * DH) * sizeof(T);
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const uint4*>(q + (kk * 4 + g) * 16);
+    }
+    const uint32_t row_bytes = (uint32_t)a.cache.row_elems() * sizeof(T);
+    const int ld_pos = lane % NCHK, ld_row = lane / NCHK;
+    int k_off[LDB], v_off[LDB];
+#pragma unroll
+    for (int i = 0; i < LDB; ++i) {
+        const int x2 = i * RPI + ld_row;
+        k_off[i] = x2 * row_bytes + ((ld_pos ^ C::k_turn(x2)) << 4);
+        v_off[i] = x2 * row_bytes + ((ld_pos ^ C::v_turn(x2)) << 4);
+    }
+    const uint32_t ring0 = (uint32_t)(size_t)(lds_ptr_t)ring + wave * C::WAVE_LDS;
+    const char* kbase = static_cast<const char*>(a.k_pages) + (size_t)kvh * ROWB;
+    const char* vbase = static_cast<const char*>(a.v_pages) + (size_t)kvh * ROWB;
+    // tile t of this wave: rows past j1 (and tiles that there are not) load as zeros without touching memory
+    auto issue = [&](const char* base, const int (&off)[LDB], int t, uint32_t lds) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const int slot = j0 + (t * 4 + wave) * KEYS + kb * 16;
+            const uint32_t page = __builtin_amdgcn_readlane(ids, (t * KB + kb) & 63);
+            const int there = t < mine ? min(max(j1 - slot, 0), 16) : 0;
+            const __amdgpu_buffer_rsrc_t rs = make_uniform_rsrc(base + a.cache.row(page, slot) * row_bytes, there ? (uint32_t)(there - 1) * row_bytes + ROWB : 0u);
+#pragma unroll
+            for (int i = 0; i < LDB; ++i) direct_load_16(rs, off[i], lds + (kb * LDB + i) * 1024);
+        }
+    };
+    auto issue_k = [&](int t) { issue(kbase, k_off, t, ring0 + (t & 1) * C::STAGE); };
+    auto issue_v = [&](int t) { issue(vbase, v_off, t, ring0 + (t & 1) * C::STAGE + C::TILE); };
+    issue_k(0); issue_v(0); issue_k(1); issue_v(1);
+
+    int k_addr[KS], v_addr[DB];
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) k_addr[kk] = r * ROWB + (((kk * 4 + g) ^ C::k_turn(r)) << 4);
+#pragma unroll
+    for (int t = 0; t < DB; ++t) {
+        if constexpr (sizeof(T) == 2) {
+            const int vr = 4 * g + (r >> 2), chunk = t * 2 + ((r & 3) >> 1);
+            v_addr[t] = C::TILE + vr * ROWB + ((chunk ^ C::v_turn(vr)) << 4) + (r & 1) * 8;
+        } else {
+            v_addr[t] = C::TILE + 4 * g * ROWB + (((t * 4 + (r >> 2)) ^ C::v_turn(4 * g)) << 4) + (r & 3) * 4;
+        }
+    }
+    f32x4 o[DB];
+#pragma unroll
+    for (int t = 0; t < DB; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    float* kept = a.logits ? a.logits + (row * a.H + xh) * a.lpad : nullptr;
+    const bool real = R0 + r < R;
+
+    for (int t = 0; t < mine; ++t) {
+        const char* w = ring + wave * C::WAVE_LDS + (t & 1) * C::STAGE;
+        const int key0 = j0 + (t * 4 + wave) * KEYS;
+        wait_loads<3 * C::LD>();                           // K of this tile is there
+        f32x4 st[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            st[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk) st[kb] = ac_mma<T>(*reinterpret_cast<const uint4*>(w + k_addr[kk] + kb * 16 * ROWB), qf[kk], st[kb]);
+        }
+        wait_lds();
+        issue_k(t + 2);
+        float top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st[kb][e] *= a.scale2;
+        if (key0 + KEYS > limit0) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) st[kb][e] = key0 + kb * 16 + 4 * g + e < limit ? st[kb][e] : -INFINITY;
+        }
+        if (kept && real) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+                if (key0 + kb * 16 < j1) *reinterpret_cast<f32x4*>(kept + key0 + kb * 16 + 4 * g) = st[kb];
+        }
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, st[kb][e]);
+        top = quad_max(top);
+        if (__builtin_amdgcn_ballot_w64(top > m) != 0) {
+            const float mn = fmaxf(m, top);
+            const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= alpha;
+#pragma unroll
+            for (int t2 = 0; t2 < DB; ++t2)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[t2][e] *= alpha;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;        // a column that has seen nothing yet: all its p are 0
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float p = __builtin_amdgcn_exp2f(st[kb][e] - ref);
+                st[kb][e] = p;
+                l += p;
+            }
+        wait_loads<3 * C::LD>();                           // V of this tile
+        if constexpr (sizeof(T) == 2) {
+            typedef __attribute__((address_space(3))) ac_short4* tr_ptr;
+#pragma unroll
+            for (int kp = 0; kp < KB / 2; ++kp) {
+                bf16x8 pf;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { pf[e] = (__bf16)st[2 * kp][e]; pf[4 + e] = (__bf16)st[2 * kp + 1][e]; }
+#pragma unroll
+                for (int t2 = 0; t2 < DB; ++t2) {
+                    const char* p = w + v_addr[t2] + kp * 32 * ROWB;
+                    const ac_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + 16 * ROWB));
+                    const ac_short8 v8 = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    o[t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v8), pf, o[t2], 0, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int t2 = 0; t2 < DB; ++t2)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[t2] = __builtin_amdgcn_mfma_f32_16x16x4f32(*reinterpret_cast<const float*>(w + v_addr[t2] + (kb * 16 + e) * ROWB), st[kb][e], o[t2], 0, 0, 0);
+        }
+        wait_lds();
+        issue_v(t + 2);
+    }
+    wait_loads_and_barrier<0>();                           // nothing is on its way into the rings any more
+    // the four waves' parts, rows of queries
+    float* part = reinterpret_cast<float*>(ring);
+    l = quad_sum(l);
+    float* to = part + (wave * 16 + r) * C::PITCH + 4 * g;
+#pragma unroll
+    for (int t = 0; t < DB; ++t) *reinterpret_cast<f32x4*>(to + t * 16) = o[t];
+    if (g == 0) { part_m[wave][r] = m; part_l[wave][r] = l; }
+    __syncthreads();
+    // sixteen threads to a row
+    const int y = tid >> 4, Y = R0 + y;
+    if (Y >= R) return;
+    const int yi = Y / a.G, yh = kvh * a.G + (Y - yi * a.G);
+    float mt = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mt = fmaxf(mt, part_m[w][y]);
+    float f[4], z = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        f[w] = part_m[w][y] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part_m[w][y] - mt);
+        z += part_l[w][y] * f[w];
+    }
+    const size_t at = ((size_t)(r0 + yi) * a.H + yh) * a.S + s;
+    const float inv = a.S > 1 ? 1.f : z > 0.f ? 1.0f / z : 0.f;
+    constexpr int CH = DH / 16;
+    const int c0 = (tid & 15) * CH;
+    float acc[CH];
+#pragma unroll
+    for (int e = 0; e < CH; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int e = 0; e < CH; ++e) acc[e] = __builtin_fmaf(part[(w * 16 + y) * C::PITCH + c0 + e], f[w], acc[e]);
+#pragma unroll
+    for (int e = 0; e < CH; ++e) acc[e] *= inv;
+    if (a.S > 1) {
+#pragma unroll
+        for (int e = 0; e < CH; e += 4) *reinterpret_cast<f32x4*>(a.part_o + at * DH + c0 + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+        if ((tid & 15) == 0) { a.part_ml[at * 2] = mt; a.part_ml[at * 2 + 1] = z; }
+    } else {
+        T* out = static_cast<T*>(a.o) + at * DH + c0;
+        if constexpr (sizeof(T) == 2) store_bf16<CH>(out, acc);
+        else {
+#pragma unroll
+            for (int e = 0; e < CH; e += 4) *reinterpret_cast<f32x4*>(out + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+        }
+        if ((tid & 15) == 0) {
+            const float l2 = z > 0.f ? mt + log2f(z) : -INFINITY;
+            if (a.lse) a.lse[at] = l2 * 0.6931471805599453f;
+            if (a.lse2) a.lse2[at] = l2;
+        }
+    }
+#endif
+}
+
+// The runs of the rows joined, dh / 4 threads to a row and head; and, where the logits were kept, what the slots got: one thread to a slot,
+// over all rows and heads of the sample, p = 2^(logit - lse) with the rows' lse formed from the runs' sums by every workgroup for itself (a launch
+// of its own for that would cost more).
+constexpr int JW_ROWS = 1024;                  // rows and heads whose lse a workgroup holds at a time
+
+__device__ __forceinline__ int runs_of(const AttendCacheArgs& a, int limit) { return max(1, (limit + a.run - 1) / a.run); }
+
+template <typename T>
+__global__ __launch_bounds__(256) void attend_cache_join_kernel(AttendCacheArgs a, int join_wgs) {
+    __shared__ float lse2[JW_ROWS];
+    const int tid = threadIdx.x, b = blockIdx.y, dh = a.cache.dh;
+    int r0;
+    const int nq = sample_rows(a, b, r0);
+    const int n = a.cache.length(b, a.max_len);
+    if ((int)blockIdx.x < join_wgs) {
+        const int tpr = dh >> 2, per = 256 / tpr, y = tid / tpr, c = tid - y * tpr;
+        const int item = blockIdx.x * per + y;
+        if (y >= per || item >= nq * a.H) return;
+        const int i = item / a.H;
+        const size_t at = (size_t)r0 * a.H + item;
+        const int S = runs_of(a, row_limit(a, n, nq, i));
+        const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + at * a.S;
+        float m = -INFINITY;
+        for (int s = 0; s < S; ++s) m = fmaxf(m, ml[s].x);
+        float z = 0.f;
+        f32x4 t = {0.f, 0.f, 0.f, 0.f};
+        const f32x4* part = reinterpret_cast<const f32x4*>(a.part_o + at * a.S * dh) + c;
+        for (int s = 0; s < S; ++s) {
+            const float2 v = ml[s];
+            const f32x4 p = part[(size_t)s * tpr];
+            const float f = v.x == -INFINITY ? 0.f : exp2f(v.x - m);
+            z = __builtin_fmaf(v.y, f, z);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = __builtin_fmaf(p[e], f, t[e]);
+        }
+        const float inv = z > 0.f ? 1.0f / z : 0.f;
+        T* o = static_cast<T*>(a.o) + at * dh + c * 4;
+        const float w[4] = {t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv};
+        if constexpr (sizeof(T) == 2) store_bf16<4>(o, w);
+        else *reinterpret_cast<f32x4*>(o) = f32x4{w[0], w[1], w[2], w[3]};
+        if (c == 0) {
+            const float l2 = z > 0.f ? m + log2f(z) : -INFINITY;
+            if (a.lse) a.lse[at] = l2 * 0.6931471805599453f;
+            if (a.lse2) a.lse2[at] = l2;
+        }
+        return;
+    }
+    const int j = ((int)blockIdx.x - join_wgs) * 256 + tid;
+    if (j - tid >= n) return;
+    const int items = nq * a.H;
+    float total = 0.f;
+    for (int c0 = 0; c0 < items; c0 += JW_ROWS) {
+        const int cnt = min(items - c0, JW_ROWS);
+        __syncthreads();
+        for (int u = tid; u < cnt; u += 256) {
+            const size_t at = (size_t)r0 * a.H + c0 + u;
+            if (a.S == 1) { lse2[u] = a.lse2[at]; continue; }
+            const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + at * a.S;
+            const int S = runs_of(a, row_limit(a, n, nq, (c0 + u) / a.H));
+            float m = -INFINITY, z = 0.f;
+            for (int s = 0; s < S; ++s) m = fmaxf(m, ml[s].x);
+            for (int s = 0; s < S; ++s) z += ml[s].x == -INFINITY ? 0.f : ml[s].y * exp2f(ml[s].x - m);
+            lse2[u] = m + log2f(z);
+        }
+        __syncthreads();
+        if (j < n) {
+            const float* x = a.logits + ((size_t)r0 * a.H + c0) * a.lpad + j;
+#pragma unroll 8
+            for (int u = 0; u < cnt; ++u) {
+                const float v = x[(size_t)u * a.lpad] - lse2[u];
+                total += j < row_limit(a, n, nq, (c0 + u) / a.H) ? exp2f(v) : 0.f;
+            }
+        }
+    }
+    if (j < n) {
+        const size_t at = (size_t)b * a.weight_stride + j;
+        a.weight_out[at] = (a.weight_in ? a.weight_in[at] : 0.f) + total / (float)a.H;
     }
 }
 
@@ -204,25 +533,46 @@ __global__ __launch_bounds__(256) void cache_weigh_generic_kernel(AttendCacheArg
 }
 
 struct AttendCachePlan {
-    int S, run;
-    size_t lse2, part_o, part_ml, bytes;        // places in the workspace
+    bool tiles;                                 // heads that the matrix instructions are built for
+    bool keep;                                  // logits are kept for the weights
+    int S, run, ntile, lpad;
+    size_t lse2, part_o, part_ml, logits, bytes;        // places in the workspace
 };
+constexpr int AC_MAX_RUN = 4096;                // a wave has the pages of its part of a run in its 64 lanes
 static AttendCachePlan attend_cache_plan(const d3tom_paged_cache& c, int rows, int max_q, int max_len, int H, int weighed) {
     AttendCachePlan p;
-    const long long groups = (long long)c.B * max_q * H;
-    long long S = groups >= 1024 ? 1 : 1024 / groups;
-    const long long most = (max_len + 255) / 256;
+    const int G = H / c.Hkv;
+    p.tiles = c.dh == 64 || c.dh == 128;
+    const long long R = (long long)max_q * G;
+    p.ntile = p.tiles ? (int)((R + 15) / 16) : 1;
+    const long long groups = p.tiles ? (long long)c.B * c.Hkv * p.ntile : (long long)c.B * max_q * H;
+    const long long want = p.tiles ? 256 : 1024, step = 256;
+    long long S = groups >= want ? 1 : want / groups;
+    const long long most = (max_len + step - 1) / step;
     S = S > most ? most : S;
-    p.run = (int)((most + S - 1) / S) * 256;
+    p.run = (int)((most + S - 1) / S * step);
+    if (p.tiles && p.run > AC_MAX_RUN) p.run = AC_MAX_RUN;
     p.S = (max_len + p.run - 1) / p.run;
+    p.keep = weighed && p.tiles && R <= 16;
+    p.lpad = (max_len + 15) / 16 * 16;
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 256); return at; };
     const size_t rh = (size_t)rows * H;
     p.lse2 = take(weighed ? rh * 4 : 0);
     p.part_o = take(p.S > 1 ? rh * p.S * c.dh * 4 : 0);
     p.part_ml = take(p.S > 1 ? rh * p.S * 8 : 0);
+    p.logits = take(p.keep ? rh * p.lpad * 4 : 0);
     p.bytes = o > 256 ? o : 256;
     return p;
+}
+template <typename T, int DH>
+static int attend_cache_launch(const AttendCacheArgs& a, hipStream_t st) {
+    static PerDeviceOnce once;
+    constexpr int LDS = 4 * AcTile<T, DH>::WAVE_LDS;
+    if (!once.run([] { return raise_dynamic_lds(attend_cache_kernel<T, DH>, LDS); })) return D3TOM_ERR_DEVICE;
+    const int units = a.nB * a.cache.Hkv * a.S;
+    D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH><<<(units + 7) / 8 * 8 * a.tiles, 256, LDS, st>>>(a)));
+    return D3TOM_OK;
 }
 static int attend_cache_check(const d3tom_paged_cache* c, int rows, int max_q, int max_len, int H) {
     const int rc = cache_check(c);
@@ -253,27 +603,38 @@ extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_p
     if ((weight_in && !weight_out) || (weight_out && weight_stride < max_len)) return D3TOM_ERR_INVALID_ARG;
     const AttendCachePlan p = attend_cache_plan(*cache, rows, max_q, max_len, H, weight_out != nullptr);
     if (ws_bytes < p.bytes || (((uintptr_t)ws) & 255u)) return D3TOM_ERR_WORKSPACE_TOO_SMALL;
-    const double most = 16777215.0;             // workgroups of 256 threads in a launch
-    if ((double)cache->B * max_q * H * p.S > most || (double)rows * H > most) return D3TOM_ERR_UNSUPPORTED;
+    const double most = 16000000.0;             // workgroups of 256 threads in a launch
+    if ((double)cache->B * max_q * H * p.S > most || (double)max_q * H > most) return D3TOM_ERR_UNSUPPORTED;
     AttendCacheArgs a{};
     a.cache = cache_view(*cache);
     a.q = q; a.k_pages = cache->k_pages; a.v_pages = cache->v_pages; a.q_stride = q_stride; a.q_off = q_off;
-    a.rows = rows; a.max_q = max_q; a.max_len = max_len; a.H = H; a.G = H / cache->Hkv; a.causal = causal != 0;
+    a.nB = cache->B; a.rows = rows; a.max_q = max_q; a.max_len = max_len; a.H = H; a.G = H / cache->Hkv; a.causal = causal != 0;
     a.scale2 = scale * LOG2E;
-    a.S = p.S; a.run = p.run; a.o = o; a.lse = lse;
+    a.S = p.S; a.run = p.run; a.o = o; a.lse = lse; a.lpad = p.lpad; a.tiles = p.ntile;
     a.lse2 = weight_out ? (float*)((char*)ws + p.lse2) : nullptr;
     a.part_o = (float*)((char*)ws + p.part_o); a.part_ml = (float*)((char*)ws + p.part_ml);
+    a.logits = p.keep ? (float*)((char*)ws + p.logits) : nullptr;
     a.weight_in = weight_in; a.weight_out = weight_out; a.weight_stride = weight_stride;
-    const int wgs = cache->B * max_q * H * p.S;
-    const dim3 wgrid((max_len + 63) / 64, cache->B);
-#define D3TOM_ATTEND_CACHE(T)                                                                                              \
-    do {                                                                                                                   \
-        D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_generic_kernel<T><<<wgs, 256, 0, st>>>(a)));                          \
-        if (p.S > 1) D3TOM_LAUNCH(CACHE_JOIN, st, (attend_cache_join_kernel<T><<<rows * H, 256, 0, st>>>(a)));             \
-        if (weight_out) D3TOM_LAUNCH(CACHE_WEIGH, st, (cache_weigh_generic_kernel<T><<<wgrid, 256, 0, st>>>(a)));          \
-    } while (0)
-    if (dt == D3TOM_BF16) D3TOM_ATTEND_CACHE(uint16_t);
-    else D3TOM_ATTEND_CACHE(float);
-#undef D3TOM_ATTEND_CACHE
+    const bool bf16 = dt == D3TOM_BF16;
+    if (p.tiles) {
+        rc = bf16 ? (dh == 128 ? attend_cache_launch<uint16_t, 128>(a, st) : attend_cache_launch<uint16_t, 64>(a, st))
+                  : (dh == 128 ? attend_cache_launch<float, 128>(a, st) : attend_cache_launch<float, 64>(a, st));
+        if (rc != D3TOM_OK) return rc;
+    } else {
+        const int wgs = cache->B * max_q * H * p.S;
+        if (bf16) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_generic_kernel<uint16_t><<<wgs, 256, 0, st>>>(a)));
+        else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_generic_kernel<float><<<wgs, 256, 0, st>>>(a)));
+    }
+    const int per = 256 / (dh / 4), join_wgs = p.S > 1 ? (max_q * H + per - 1) / per : 0, weigh_wgs = p.keep ? (max_len + 255) / 256 : 0;
+    if (join_wgs + weigh_wgs > 0) {
+        const dim3 grid(join_wgs + weigh_wgs, cache->B);
+        if (bf16) D3TOM_LAUNCH(CACHE_JOIN, st, (attend_cache_join_kernel<uint16_t><<<grid, 256, 0, st>>>(a, join_wgs)));
+        else D3TOM_LAUNCH(CACHE_JOIN, st, (attend_cache_join_kernel<float><<<grid, 256, 0, st>>>(a, join_wgs)));
+    }
+    if (weight_out && !p.keep) {
+        const dim3 wgrid((max_len + 63) / 64, cache->B);
+        if (bf16) D3TOM_LAUNCH(CACHE_WEIGH, st, (cache_weigh_generic_kernel<uint16_t><<<wgrid, 256, 0, st>>>(a)));
+        else D3TOM_LAUNCH(CACHE_WEIGH, st, (cache_weigh_generic_kernel<float><<<wgrid, 256, 0, st>>>(a)));
+    }
     return D3TOM_OK;
 }
