@@ -412,6 +412,310 @@ __global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a)
 #endif
 }
 
+
+// More than 16 rows to a key head: the waves share the tiles and have QB blocks of 16 rows each, so that a key's row is read from LDS four times
+// and from memory once for 64 QB rows.  Tiles of 16 KB of K and of V, of which every wave loads a quarter, in a ring of two stages; two
+// workgroups to a compute unit, so that one's exponentials run beside the other's matrix instructions.
+template <typename T, int DH> struct AcShared {
+    using C = AcTile<T, DH>;
+    static constexpr int TILE = 16384, KEYS = TILE / C::ROWB, KB = KEYS / 16, LD = 4, STAGE = 2 * TILE, LDS = 2 * STAGE;
+    static constexpr int PAGES = 256;                  // blocks of 16 slots of a run whose pages lie in LDS
+};
+template <typename T, int DH, int QB>
+__global__ __launch_bounds__(256, 2) void attend_cache_rows_kernel(AttendCacheArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    using C = AcTile<T, DH>;
+    using W = AcShared<T, DH>;
+    constexpr int ROWB = C::ROWB, NCHK = C::NCHK, KEYS = W::KEYS, KB = W::KB, LD = W::LD, RPI = C::RPI, KS = C::KS, DB = C::DB;
+    extern __shared__ __attribute__((aligned(16))) char ring[];
+    __shared__ uint32_t pages[W::PAGES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    int id = blockIdx.x;
+    const int xcd = id & 7;
+    id >>= 3;
+    const int tile = id % a.tiles;
+    int unit = (id / a.tiles) * 8 + xcd;
+    const int s = unit % a.S; unit /= a.S;
+    const int kvh = unit % a.cache.Hkv, b = unit / a.cache.Hkv;
+    if (b >= a.nB) return;
+    int r0;
+    const int nq = sample_rows(a, b, r0);
+    constexpr int ROWS = 64 * QB;
+    const int R = nq * a.G, R0 = tile * ROWS;
+    if (R0 >= R) return;
+    const int n = a.cache.length(b, a.max_len);
+    const int j0 = s * a.run, j1 = min(row_limit(a, n, nq, (min(R0 + ROWS, R) - 1) / a.G), j0 + a.run);
+    if (j0 >= j1 && s > 0) return;
+    const int W0 = R0 + wave * 16 * QB;                // this wave's first row
+    const bool works = W0 < R;
+    size_t row[QB];
+    int xh[QB], limit[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int x = min(W0 + qb * 16 + r, R - 1), xi = x / a.G;
+        xh[qb] = kvh * a.G + (x - xi * a.G);
+        row[qb] = (size_t)(r0 + xi);
+        limit[qb] = min(row_limit(a, n, nq, xi), j1);
+    }
+    const int limit0 = min(row_limit(a, n, nq, min(W0, R - 1) / a.G), j1);
+    const int ntile = j1 > j0 ? (j1 - j0 + KEYS - 1) / KEYS : 0;
+    {
+        const int slot = j0 + tid * 16;
+        pages[tid] = slot < j1 ? a.cache.readable(a.cache.page_of(b, slot)) : 0u;
+    }
+    uint4 qf[QB][KS];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const char* q = static_cast<const char*>(a.q) + (row[qb] * a.q_stride + (size_t)xh[qb] * DH) * sizeof(T);
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) qf[qb][kk] = *reinterpret_cast<const uint4*>(q + (kk * 4 + g) * 16);
+    }
+    const uint32_t row_bytes = (uint32_t)a.cache.row_elems() * sizeof(T);
+    const int ld_pos = lane % NCHK, ld_row = lane / NCHK;
+    const uint32_t ring0 = (uint32_t)(size_t)(lds_ptr_t)ring;
+    const char* kbase = static_cast<const char*>(a.k_pages) + (size_t)kvh * ROWB;
+    const char* vbase = static_cast<const char*>(a.v_pages) + (size_t)kvh * ROWB;
+    int k_off[LD], v_off[LD];                          // of the row inside its block of 16
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+        const int x = ((wave * LD + i) * RPI + ld_row) & 15;
+        k_off[i] = x * row_bytes + ((ld_pos ^ C::k_turn(x)) << 4);
+        v_off[i] = x * row_bytes + ((ld_pos ^ C::v_turn(x)) << 4);
+    }
+    // this wave's loads of tile t; `ids`: lane i has the page of the tile's block i
+    auto issue = [&](int t, uint32_t ids) {
+        const uint32_t lds = ring0 + (t & 1) * W::STAGE + wave * LD * 1024;
+#pragma unroll
+        for (int i = 0; i < LD; ++i) {
+            const int kb = (wave * LD + i) * RPI / 16, slot = j0 + t * KEYS + kb * 16;
+            const uint32_t page = __builtin_amdgcn_readlane(ids, kb);
+            const int there = min(max(j1 - slot, 0), 16);
+            const uint32_t bytes = there ? (uint32_t)(there - 1) * row_bytes + ROWB : 0u;
+            const size_t at = a.cache.row(page, slot) * row_bytes;
+            direct_load_16(make_uniform_rsrc(kbase + at, bytes), k_off[i], lds + i * 1024);
+            direct_load_16(make_uniform_rsrc(vbase + at, bytes), v_off[i], lds + W::TILE + i * 1024);
+        }
+    };
+    auto pages_of = [&](int t) { return pages[min(t * KB + (lane & (KB - 1)), W::PAGES - 1)]; };
+    __syncthreads();
+    issue(0, pages_of(0));
+    issue(1, pages_of(1));
+
+    int k_addr[KS], v_addr[DB];
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) k_addr[kk] = r * ROWB + (((kk * 4 + g) ^ C::k_turn(r)) << 4);
+#pragma unroll
+    for (int t = 0; t < DB; ++t) {
+        if constexpr (sizeof(T) == 2) {
+            const int vr = 4 * g + (r >> 2), chunk = t * 2 + ((r & 3) >> 1);
+            v_addr[t] = W::TILE + vr * ROWB + ((chunk ^ C::v_turn(vr)) << 4) + (r & 1) * 8;
+        } else {
+            v_addr[t] = W::TILE + 4 * g * ROWB + (((t * 4 + (r >> 2)) ^ C::v_turn(4 * g)) << 4) + (r & 3) * 4;
+        }
+    }
+    f32x4 o[QB][DB];
+    float m[QB], l[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        m[qb] = -INFINITY; l[qb] = 0.f;
+#pragma unroll
+        for (int t = 0; t < DB; ++t) o[qb][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int t = 0; t < ntile; ++t) {
+        wait_loads_and_barrier<2 * LD>();              // everybody's part of this tile is there
+        const char* w = ring + (t & 1) * W::STAGE;
+        const int key0 = j0 + t * KEYS;
+        const uint32_t ids = pages_of(t + 2);
+        if (works) {
+            f32x4 st[QB][KB];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) st[qb][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk) {
+                    const uint4 kf = *reinterpret_cast<const uint4*>(w + k_addr[kk] + kb * 16 * ROWB);
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb) st[qb][kb] = ac_mma<T>(kf, qf[qb][kk], st[qb][kb]);
+                }
+            }
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) st[qb][kb][e] *= a.scale2;
+                if (key0 + KEYS > limit0) {
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) st[qb][kb][e] = key0 + kb * 16 + 4 * g + e < limit[qb] ? st[qb][kb][e] : -INFINITY;
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, st[qb][kb][e]);
+                top = quad_max(top);
+                if (__builtin_amdgcn_ballot_w64(top > m[qb]) != 0) {
+                    const float mn = fmaxf(m[qb], top);
+                    const float alpha = m[qb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[qb] - mn);
+                    m[qb] = mn;
+                    l[qb] *= alpha;
+#pragma unroll
+                    for (int t2 = 0; t2 < DB; ++t2)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[qb][t2][e] *= alpha;
+                }
+                const float ref = m[qb] == -INFINITY ? 0.f : m[qb];
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(st[qb][kb][e] - ref);
+                        st[qb][kb][e] = p;
+                        l[qb] += p;
+                    }
+            }
+            if constexpr (sizeof(T) == 2) {
+                typedef __attribute__((address_space(3))) ac_short4* tr_ptr;
+#pragma unroll
+                for (int kp = 0; kp < KB / 2; ++kp) {
+                    bf16x8 pf[QB];
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { pf[qb][e] = (__bf16)st[qb][2 * kp][e]; pf[qb][4 + e] = (__bf16)st[qb][2 * kp + 1][e]; }
+#pragma unroll
+                    for (int t2 = 0; t2 < DB; ++t2) {
+                        const char* p = w + v_addr[t2] + kp * 32 * ROWB;
+                        const ac_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + 16 * ROWB));
+                        const ac_short8 v8 = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                        for (int qb = 0; qb < QB; ++qb) o[qb][t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v8), pf[qb], o[qb][t2], 0, 0, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int t2 = 0; t2 < DB; ++t2)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float v = *reinterpret_cast<const float*>(w + v_addr[t2] + (kb * 16 + e) * ROWB);
+#pragma unroll
+                            for (int qb = 0; qb < QB; ++qb) o[qb][t2] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, st[qb][kb][e], o[qb][t2], 0, 0, 0);
+                        }
+            }
+        }
+        wait_lds();
+        phase_barrier();                               // everybody has read this tile
+        issue(t + 2, ids);
+    }
+    wait_loads<0>();                                   // nothing is on its way into LDS when the workgroup ends
+    if (!works) return;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        if (W0 + qb * 16 + r >= R) continue;
+        const float z = quad_sum(l[qb]);
+        const size_t at = (row[qb] * a.H + xh[qb]) * a.S + s;
+        const float inv = a.S > 1 ? 1.f : z > 0.f ? 1.0f / z : 0.f;
+#pragma unroll
+        for (int t = 0; t < DB; ++t) {
+            const f32x4 v = {o[qb][t][0] * inv, o[qb][t][1] * inv, o[qb][t][2] * inv, o[qb][t][3] * inv};
+            const size_t to = at * DH + t * 16 + 4 * g;
+            if (a.S > 1) *reinterpret_cast<f32x4*>(a.part_o + to) = v;
+            else if constexpr (sizeof(T) == 2) { const float w4[4] = {v[0], v[1], v[2], v[3]}; store_bf16<4>(static_cast<T*>(a.o) + to, w4); }
+            else *reinterpret_cast<f32x4*>(static_cast<T*>(a.o) + to) = v;
+        }
+        if (g == 0) {
+            if (a.S > 1) { a.part_ml[at * 2] = m[qb]; a.part_ml[at * 2 + 1] = z; }
+            else {
+                const float l2 = z > 0.f ? m[qb] + log2f(z) : -INFINITY;
+                if (a.lse) a.lse[at] = l2 * 0.6931471805599453f;
+                if (a.lse2) a.lse2[at] = l2;
+            }
+        }
+    }
+#endif
+}
+
+// What the slots got where the logits are not kept: they are formed again, K Q^T once more (the keys' rows a third time through memory is less than
+// 4 bytes a logit there and back).  A workgroup has a tile of a sample's slots and goes over all heads and rows, wave w over key heads w, w + 8, ...
+// (or parts of a head's rows where there are fewer); the keys of a head lie in its registers, the queries come from the caches.
+constexpr int CW_WAVES = 8;
+template <typename T, int DH>
+__global__ __launch_bounds__(CW_WAVES * 64) void cache_weigh_kernel(AttendCacheArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    using C = AcTile<T, DH>;
+    constexpr int KS = C::KS, KB = C::KS > 4 ? 2 : 4, KEYS = KB * 16;
+    __shared__ float sums[CW_WAVES][KEYS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    const int b = blockIdx.y;
+    const int n = a.cache.length(b, a.max_len), key0 = blockIdx.x * KEYS;
+    if (key0 >= n) return;
+    int r0;
+    const int nq = sample_rows(a, b, r0), R = nq * a.G;
+    const size_t row_bytes = a.cache.row_elems() * sizeof(T);
+    const char* kp[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+        const int j = min(key0 + kb * 16 + r, n - 1);
+        kp[kb] = static_cast<const char*>(a.k_pages) + a.cache.row(a.cache.readable(a.cache.page_of(b, j)), j) * row_bytes + g * 16;
+    }
+    f32x4 acc[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) acc[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int parts = a.cache.Hkv >= CW_WAVES ? 1 : (CW_WAVES + a.cache.Hkv - 1) / a.cache.Hkv;
+    for (int it = wave; it < a.cache.Hkv * parts; it += CW_WAVES) {
+        const int kvh = it / parts, part = it - kvh * parts;
+        if (part * 16 >= R) continue;
+        uint4 kf[KB][KS];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk) kf[kb][kk] = *reinterpret_cast<const uint4*>(kp[kb] + (size_t)kvh * C::ROWB + kk * 64);
+        for (int x0 = part * 16; x0 < R; x0 += parts * 16) {
+            const int x = min(x0 + r, R - 1), xi = x / a.G, xh = kvh * a.G + (x - xi * a.G);
+            const size_t row = (size_t)(r0 + xi);
+            const char* q = static_cast<const char*>(a.q) + (row * a.q_stride + (size_t)xh * DH) * sizeof(T) + g * 16;
+            const float lse2 = a.lse2[row * a.H + xh];
+            const int limit = x0 + r < R ? row_limit(a, n, nq, xi) : 0;
+            uint4 qf[KS];
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const uint4*>(q + kk * 64);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                f32x4 st = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk) st = ac_mma<T>(kf[kb][kk], qf[kk], st);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(st[e] * a.scale2 - lse2);
+                    acc[kb][e] += key0 + kb * 16 + 4 * g + e < limit ? p : 0.f;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float v = row16_sum(acc[kb][e]);
+            if (r == 0) sums[wave][kb * 16 + 4 * g + e] = v;
+        }
+    __syncthreads();
+    const int j = key0 + tid;
+    if (tid < KEYS && j < n) {
+        float total = 0.f;
+#pragma unroll
+        for (int w = 0; w < CW_WAVES; ++w) total += sums[w][tid];
+        const size_t at = (size_t)b * a.weight_stride + j;
+        a.weight_out[at] = (a.weight_in ? a.weight_in[at] : 0.f) + total / (float)a.H;
+    }
+#endif
+}
+
 // The runs of the rows joined, dh / 4 threads to a row and head; and, where the logits were kept, what the slots got: one thread to a slot,
 // over all rows and heads of the sample, p = 2^(logit - lse) with the rows' lse formed from the runs' sums by every workgroup for itself (a launch
 // of its own for that would cost more).
@@ -532,28 +836,32 @@ __global__ __launch_bounds__(256) void cache_weigh_generic_kernel(AttendCacheArg
     }
 }
 
+// How a call goes: a rule on host-known sizes only.
+//   heads of 64 and 128   up to 16 rows to a key head: waves on their own, a run for every compute unit
+//                         more: 64 or 128 rows that share tiles, two workgroups to a unit
+//   others                a workgroup per row, head and run
+enum { AC_GENERIC = 0, AC_WAVES, AC_ROWS64, AC_ROWS128 };
 struct AttendCachePlan {
-    bool tiles;                                 // heads that the matrix instructions are built for
+    int kernel;
     bool keep;                                  // logits are kept for the weights
-    int S, run, ntile, lpad;
+    int S, run, tiles, lpad;
     size_t lse2, part_o, part_ml, logits, bytes;        // places in the workspace
 };
-constexpr int AC_MAX_RUN = 4096;                // a wave has the pages of its part of a run in its 64 lanes
+constexpr int AC_MAX_RUN = 4096;                // the pages of a run: in a wave's 64 lanes for each quarter, or 256 words of LDS
 static AttendCachePlan attend_cache_plan(const d3tom_paged_cache& c, int rows, int max_q, int max_len, int H, int weighed) {
     AttendCachePlan p;
-    const int G = H / c.Hkv;
-    p.tiles = c.dh == 64 || c.dh == 128;
-    const long long R = (long long)max_q * G;
-    p.ntile = p.tiles ? (int)((R + 15) / 16) : 1;
-    const long long groups = p.tiles ? (long long)c.B * c.Hkv * p.ntile : (long long)c.B * max_q * H;
-    const long long want = p.tiles ? 256 : 1024, step = 256;
-    long long S = groups >= want ? 1 : want / groups;
+    const long long R = (long long)max_q * (H / c.Hkv);
+    p.kernel = c.dh != 64 && c.dh != 128 ? AC_GENERIC : R <= 16 ? AC_WAVES : R <= 64 ? AC_ROWS64 : AC_ROWS128;
+    const int tile_rows[] = {1, 16, 64, 128}, want[] = {1024, 256, 512, 512};
+    p.tiles = (int)((R + tile_rows[p.kernel] - 1) / tile_rows[p.kernel]);
+    const long long groups = (long long)c.B * (p.kernel == AC_GENERIC ? (long long)max_q * H : (long long)c.Hkv * p.tiles), step = 256;
+    long long S = groups >= want[p.kernel] ? 1 : want[p.kernel] / groups;
     const long long most = (max_len + step - 1) / step;
     S = S > most ? most : S;
     p.run = (int)((most + S - 1) / S * step);
-    if (p.tiles && p.run > AC_MAX_RUN) p.run = AC_MAX_RUN;
+    if (p.kernel != AC_GENERIC && p.run > AC_MAX_RUN) p.run = AC_MAX_RUN;
     p.S = (max_len + p.run - 1) / p.run;
-    p.keep = weighed && p.tiles && R <= 16;
+    p.keep = weighed && p.kernel == AC_WAVES;
     p.lpad = (max_len + 15) / 16 * 16;
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 256); return at; };
@@ -566,12 +874,24 @@ static AttendCachePlan attend_cache_plan(const d3tom_paged_cache& c, int rows, i
     return p;
 }
 template <typename T, int DH>
-static int attend_cache_launch(const AttendCacheArgs& a, hipStream_t st) {
+static int attend_cache_launch(const AttendCacheArgs& a, int kernel, hipStream_t st) {
     static PerDeviceOnce once;
-    constexpr int LDS = 4 * AcTile<T, DH>::WAVE_LDS;
-    if (!once.run([] { return raise_dynamic_lds(attend_cache_kernel<T, DH>, LDS); })) return D3TOM_ERR_DEVICE;
-    const int units = a.nB * a.cache.Hkv * a.S;
-    D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH><<<(units + 7) / 8 * 8 * a.tiles, 256, LDS, st>>>(a)));
+    constexpr int WAVES_LDS = 4 * AcTile<T, DH>::WAVE_LDS, ROWS_LDS = AcShared<T, DH>::LDS;
+    if (!once.run([] {
+            return raise_dynamic_lds(attend_cache_kernel<T, DH>, WAVES_LDS) && raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 1>, ROWS_LDS) &&
+                   raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 2>, ROWS_LDS);
+        })) return D3TOM_ERR_DEVICE;
+    const int wgs = (a.nB * a.cache.Hkv * a.S + 7) / 8 * 8 * a.tiles;
+    if (kernel == AC_WAVES) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH><<<wgs, 256, WAVES_LDS, st>>>(a)));
+    else if (kernel == AC_ROWS64) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, 1><<<wgs, 256, ROWS_LDS, st>>>(a)));
+    else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, 2><<<wgs, 256, ROWS_LDS, st>>>(a)));
+    return D3TOM_OK;
+}
+template <typename T, int DH>
+static int cache_weigh_launch(const AttendCacheArgs& a, hipStream_t st) {
+    constexpr int KEYS = AcTile<T, DH>::KS > 4 ? 32 : 64;
+    const dim3 grid((a.max_len + KEYS - 1) / KEYS, a.nB);
+    D3TOM_LAUNCH(CACHE_WEIGH, st, (cache_weigh_kernel<T, DH><<<grid, CW_WAVES * 64, 0, st>>>(a)));
     return D3TOM_OK;
 }
 static int attend_cache_check(const d3tom_paged_cache* c, int rows, int max_q, int max_len, int H) {
@@ -610,15 +930,15 @@ extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_p
     a.q = q; a.k_pages = cache->k_pages; a.v_pages = cache->v_pages; a.q_stride = q_stride; a.q_off = q_off;
     a.nB = cache->B; a.rows = rows; a.max_q = max_q; a.max_len = max_len; a.H = H; a.G = H / cache->Hkv; a.causal = causal != 0;
     a.scale2 = scale * LOG2E;
-    a.S = p.S; a.run = p.run; a.o = o; a.lse = lse; a.lpad = p.lpad; a.tiles = p.ntile;
+    a.S = p.S; a.run = p.run; a.o = o; a.lse = lse; a.lpad = p.lpad; a.tiles = p.tiles;
     a.lse2 = weight_out ? (float*)((char*)ws + p.lse2) : nullptr;
     a.part_o = (float*)((char*)ws + p.part_o); a.part_ml = (float*)((char*)ws + p.part_ml);
     a.logits = p.keep ? (float*)((char*)ws + p.logits) : nullptr;
     a.weight_in = weight_in; a.weight_out = weight_out; a.weight_stride = weight_stride;
     const bool bf16 = dt == D3TOM_BF16;
-    if (p.tiles) {
-        rc = bf16 ? (dh == 128 ? attend_cache_launch<uint16_t, 128>(a, st) : attend_cache_launch<uint16_t, 64>(a, st))
-                  : (dh == 128 ? attend_cache_launch<float, 128>(a, st) : attend_cache_launch<float, 64>(a, st));
+    if (p.kernel != AC_GENERIC) {
+        rc = bf16 ? (dh == 128 ? attend_cache_launch<uint16_t, 128>(a, p.kernel, st) : attend_cache_launch<uint16_t, 64>(a, p.kernel, st))
+                  : (dh == 128 ? attend_cache_launch<float, 128>(a, p.kernel, st) : attend_cache_launch<float, 64>(a, p.kernel, st));
         if (rc != D3TOM_OK) return rc;
     } else {
         const int wgs = cache->B * max_q * H * p.S;
@@ -631,7 +951,10 @@ extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_p
         if (bf16) D3TOM_LAUNCH(CACHE_JOIN, st, (attend_cache_join_kernel<uint16_t><<<grid, 256, 0, st>>>(a, join_wgs)));
         else D3TOM_LAUNCH(CACHE_JOIN, st, (attend_cache_join_kernel<float><<<grid, 256, 0, st>>>(a, join_wgs)));
     }
-    if (weight_out && !p.keep) {
+    if (weight_out && !p.keep && p.kernel != AC_GENERIC) {
+        return bf16 ? (dh == 128 ? cache_weigh_launch<uint16_t, 128>(a, st) : cache_weigh_launch<uint16_t, 64>(a, st))
+                    : (dh == 128 ? cache_weigh_launch<float, 128>(a, st) : cache_weigh_launch<float, 64>(a, st));
+    } else if (weight_out && !p.keep) {
         const dim3 wgrid((max_len + 63) / 64, cache->B);
         if (bf16) D3TOM_LAUNCH(CACHE_WEIGH, st, (cache_weigh_generic_kernel<uint16_t><<<wgrid, 256, 0, st>>>(a)));
         else D3TOM_LAUNCH(CACHE_WEIGH, st, (cache_weigh_generic_kernel<float><<<wgrid, 256, 0, st>>>(a)));
