@@ -449,6 +449,23 @@ def test_cache_evict_protects_by_number(B):
     assert OC.evict(w[0], tok[0], 4, 1, 2).tolist() == src[0, :4].tolist() == [0, 1, 4, 3]
 
 
+def test_cache_evict_weights_of_any_bits(B):
+    # NaN weights (outside the contract) still leave keep slots, every one a row of its own
+    rng = np.random.default_rng(9)
+    c = Cache(B, [3000], 1, 8, 16, "bf16", seed=0)
+    w = torch.from_numpy(rng.integers(-2 ** 31, 2 ** 31, (1, 3000)).astype(np.int32)).cuda()
+    w[0, ::7] = -1                                                # all bits
+    w[0, 1::7] = 0x7FFFFFFF
+    src, left, tok = torch.full((1, 3000), -3, dtype=torch.int32, device="cuda"), _i32([0]), _i32(rng.permutation(3000)[None])
+    for keep in (1, 200, 430, 1500, 2999):
+        B.d3tom_cache_evict(c.handle, 3000, _i32([keep]), 3, 11, w.view(torch.float32), tok, torch.zeros(1, 3000, device="cuda"), torch.zeros_like(tok), left,
+                            B.workspace(B.d3tom_cache_evict_workspace_bytes(c.handle, 3000)), src=src)
+        got = src[0, :keep].cpu().numpy()
+        assert int(left[0]) == keep and len(set(got.tolist())) == keep and got.min() >= 0 and got.max() < 3000
+        moved = got != np.arange(keep)
+        assert (got[moved] >= keep).all() and (np.diff(got[moved]) > 0).all()
+
+
 # ---- together ---------------------------------------------------------------------------------------------------------------------------
 class Model:
     """One layer's cache as a program uses it: append, attend with weights, evict when a sample is over its budget."""
