@@ -716,41 +716,83 @@ __global__ __launch_bounds__(CW_WAVES * 64) void cache_weigh_kernel(AttendCacheA
 #endif
 }
 
-// The runs of the rows joined, dh / 4 threads to a row and head; and, where the logits were kept, what the slots got: one thread to a slot,
-// over all rows and heads of the sample, p = 2^(logit - lse) with the rows' lse formed from the runs' sums by every workgroup for itself (a launch
-// of its own for that would cost more).
+// The runs of the rows joined: dh / 4 threads to a row and head, and `groups` such groups of threads that have every groups-th run, so that few
+// runs are one trip to memory; they meet in LDS.  And, where the logits were kept, what the slots got: one thread to a slot, over all rows and heads of the sample,
+// p = 2^(logit - lse), with the rows' lse formed from the runs' sums by every workgroup for itself, eight threads to a row (a launch of its own for
+// that would cost more).
 constexpr int JW_ROWS = 1024;                  // rows and heads whose lse a workgroup holds at a time
+constexpr int JW_UNROLL = 4;                   // runs requested at once
 
 __device__ __forceinline__ int runs_of(const AttendCacheArgs& a, int limit) { return max(1, (limit + a.run - 1) / a.run); }
 
 template <typename T>
-__global__ __launch_bounds__(256) void attend_cache_join_kernel(AttendCacheArgs a, int join_wgs) {
+__global__ __launch_bounds__(256) void attend_cache_join_kernel(AttendCacheArgs a, int join_wgs, int groups) {
     __shared__ float lse2[JW_ROWS];
+    __shared__ float gm[64], gz[64];
+    __shared__ __attribute__((aligned(16))) f32x4 gt[256];
     const int tid = threadIdx.x, b = blockIdx.y, dh = a.cache.dh;
     int r0;
     const int nq = sample_rows(a, b, r0);
     const int n = a.cache.length(b, a.max_len);
     if ((int)blockIdx.x < join_wgs) {
-        const int tpr = dh >> 2, per = 256 / tpr, y = tid / tpr, c = tid - y * tpr;
-        const int item = blockIdx.x * per + y;
-        if (y >= per || item >= nq * a.H) return;
-        const int i = item / a.H;
+        const int tpr = dh >> 2, per = 256 / tpr / groups, y = tid / tpr, c = tid - y * tpr;
+        const int which = y / groups, g = y - which * groups, item = blockIdx.x * per + which;
+        const bool there = which < per && item < nq * a.H;
         const size_t at = (size_t)r0 * a.H + item;
-        const int S = runs_of(a, row_limit(a, n, nq, i));
-        const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + at * a.S;
-        float m = -INFINITY;
-        for (int s = 0; s < S; ++s) m = fmaxf(m, ml[s].x);
-        float z = 0.f;
+        float m = -INFINITY, z = 0.f;
         f32x4 t = {0.f, 0.f, 0.f, 0.f};
-        const f32x4* part = reinterpret_cast<const f32x4*>(a.part_o + at * a.S * dh) + c;
-        for (int s = 0; s < S; ++s) {
-            const float2 v = ml[s];
-            const f32x4 p = part[(size_t)s * tpr];
-            const float f = v.x == -INFINITY ? 0.f : exp2f(v.x - m);
-            z = __builtin_fmaf(v.y, f, z);
+        if (there) {
+            const int S = runs_of(a, row_limit(a, n, nq, item / a.H));
+            const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + at * a.S;
+            const f32x4* part = reinterpret_cast<const f32x4*>(a.part_o + at * a.S * dh) + c;
+            for (int s = g; s < S; s += groups * JW_UNROLL) {
+                float2 v[JW_UNROLL];
+                f32x4 p[JW_UNROLL];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = __builtin_fmaf(p[e], f, t[e]);
+                for (int u = 0; u < JW_UNROLL; ++u) {
+                    const int su = min(s + u * groups, S - 1);
+                    v[u] = ml[su];
+                    p[u] = part[(size_t)su * tpr];
+                }
+                float mn = m;
+#pragma unroll
+                for (int u = 0; u < JW_UNROLL; ++u) mn = fmaxf(mn, v[u].x);             // (a run that comes twice does not change it)
+                const float ref = mn == -INFINITY ? 0.f : mn, f0 = exp2f(m - ref);
+                m = mn;
+                z *= f0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] *= f0;
+#pragma unroll
+                for (int u = 0; u < JW_UNROLL; ++u) {
+                    const float f = s + u * groups < S ? exp2f(v[u].x - ref) : 0.f;
+                    z = __builtin_fmaf(v[u].y, f, z);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t[e] = __builtin_fmaf(p[u][e], f, t[e]);
+                }
+            }
         }
+        if (groups > 1) {
+            gt[tid] = t;
+            if (c == 0 && y < 64) { gm[y] = m; gz[y] = z; }
+            __syncthreads();
+            if (there && g == 0) {
+                float mt = m;
+                for (int i = 1; i < groups; ++i) mt = fmaxf(mt, gm[y + i]);
+                const float ref = mt == -INFINITY ? 0.f : mt, f0 = exp2f(m - ref);
+                z *= f0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] *= f0;
+                for (int i = 1; i < groups; ++i) {
+                    const float f = exp2f(gm[y + i] - ref);
+                    const f32x4 p = gt[tid + i * tpr];
+                    z = __builtin_fmaf(gz[y + i], f, z);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t[e] = __builtin_fmaf(p[e], f, t[e]);
+                }
+                m = mt;
+            }
+        }
+        if (!there || g != 0) return;
         const float inv = z > 0.f ? 1.0f / z : 0.f;
         T* o = static_cast<T*>(a.o) + at * dh + c * 4;
         const float w[4] = {t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv};
@@ -770,15 +812,23 @@ __global__ __launch_bounds__(256) void attend_cache_join_kernel(AttendCacheArgs 
     for (int c0 = 0; c0 < items; c0 += JW_ROWS) {
         const int cnt = min(items - c0, JW_ROWS);
         __syncthreads();
-        for (int u = tid; u < cnt; u += 256) {
-            const size_t at = (size_t)r0 * a.H + c0 + u;
-            if (a.S == 1) { lse2[u] = a.lse2[at]; continue; }
-            const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + at * a.S;
-            const int S = runs_of(a, row_limit(a, n, nq, (c0 + u) / a.H));
-            float m = -INFINITY, z = 0.f;
-            for (int s = 0; s < S; ++s) m = fmaxf(m, ml[s].x);
-            for (int s = 0; s < S; ++s) z += ml[s].x == -INFINITY ? 0.f : ml[s].y * exp2f(ml[s].x - m);
-            lse2[u] = m + log2f(z);
+        if (a.S == 1) {
+            for (int u = tid; u < cnt; u += 256) lse2[u] = a.lse2[(size_t)r0 * a.H + c0 + u];
+        } else {
+            const int sub = tid & 7;
+            for (int u = tid >> 3; u < (cnt + 31) / 32 * 32; u += 32) {
+                const int uc = min(u, cnt - 1);
+                const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + ((size_t)r0 * a.H + c0 + uc) * a.S;
+                const int S = runs_of(a, row_limit(a, n, nq, (c0 + uc) / a.H));
+                float m = -INFINITY, z = 0.f;
+                for (int s = sub; s < S; s += 8) lse2_combine(m, z, ml[s].x, ml[s].y);
+#pragma unroll
+                for (int o = 1; o < 8; o <<= 1) {
+                    const float m2 = __shfl_xor(m, o), z2 = __shfl_xor(z, o);
+                    lse2_combine(m, z, m2, z2);
+                }
+                if (sub == 0 && u < cnt) lse2[u] = m + log2f(z);
+            }
         }
         __syncthreads();
         if (j < n) {
@@ -945,11 +995,13 @@ extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_p
         if (bf16) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_generic_kernel<uint16_t><<<wgs, 256, 0, st>>>(a)));
         else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_generic_kernel<float><<<wgs, 256, 0, st>>>(a)));
     }
-    const int per = 256 / (dh / 4), join_wgs = p.S > 1 ? (max_q * H + per - 1) / per : 0, weigh_wgs = p.keep ? (max_len + 255) / 256 : 0;
+    int groups = 1;                              // of threads, over the runs of a row
+    while (groups < p.S && groups * 2 <= 256 / (dh / 4)) groups *= 2;
+    const int per = 256 / (dh / 4) / groups, join_wgs = p.S > 1 ? (max_q * H + per - 1) / per : 0, weigh_wgs = p.keep ? (max_len + 255) / 256 : 0;
     if (join_wgs + weigh_wgs > 0) {
         const dim3 grid(join_wgs + weigh_wgs, cache->B);
-        if (bf16) D3TOM_LAUNCH(CACHE_JOIN, st, (attend_cache_join_kernel<uint16_t><<<grid, 256, 0, st>>>(a, join_wgs)));
-        else D3TOM_LAUNCH(CACHE_JOIN, st, (attend_cache_join_kernel<float><<<grid, 256, 0, st>>>(a, join_wgs)));
+        if (bf16) D3TOM_LAUNCH(CACHE_JOIN, st, (attend_cache_join_kernel<uint16_t><<<grid, 256, 0, st>>>(a, join_wgs, groups)));
+        else D3TOM_LAUNCH(CACHE_JOIN, st, (attend_cache_join_kernel<float><<<grid, 256, 0, st>>>(a, join_wgs, groups)));
     }
     if (weight_out && !p.keep && p.kernel != AC_GENERIC) {
         return bf16 ? (dh == 128 ? cache_weigh_launch<uint16_t, 128>(a, st) : cache_weigh_launch<uint16_t, 64>(a, st))

@@ -424,7 +424,7 @@ def _evict_case(B, dtype, Hkv, dh, page, lens, keep, first, recent, seed=0, leve
     ("bf16", 2, 64, 16, [1], [1], 0, 0), ("bf16", 2, 64, 16, [1], [0], 3, 3), ("bf16", 2, 64, 16, [100, 37, 0, 64], [40, 36, 5, 64], 4, 8), ("bf16", 8, 128, 64, [300, 299], [1, 298], 0, 20),
     ("f32", 1, 4, 16, [50, 51], [25, 60], 2, 2), ("f32", 3, 20, 32, [1000], [500], 0, 0), ("bf16", 1, 8, 16, [5000, 17, 1025], [3333, 9, 1024], 10, 100),
     ("bf16", 1, 8, 16, [2048, 1023, 1024, 1025], [1024, 512, 1, 1000], 4, 64), ("bf16", 1, 16, 128, [30000], [11111], 4, 3000), ("bf16", 2, 64, 16, [90, 80], [-4, 10], 50, 60),
-    ("bf16", 1, 8, 4096, [70001], [35000], 4, 64)])
+    ("bf16", 1, 8, 4096, [70001], [35000], 4, 64), ("bf16", 1, 8, 4096, [66000, 300, 33333, 0], [65000, 299, 3, 0], 4, 64), ("bf16", 1, 8, 64, [200003], [123456], 4, 5000)])
 @pytest.mark.parametrize("aliased", [False, True])
 def test_cache_evict(B, dtype, Hkv, dh, page, lens, keep, first, recent, aliased):
     _evict_case(B, dtype, Hkv, dh, page, lens, keep, first, recent, aliased=aliased)
