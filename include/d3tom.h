@@ -533,7 +533,8 @@ int d3tom_cache_append(const d3tom_paged_cache* cache /* host */, const void* k,
  * bf16: the probabilities enter the product with v as bf16, relative to the running maximum of their row, all sums are float32.
  * Long caches are cut into runs of slots whose results are joined; how goes by the host-known sizes only, so that a call has
  * the same bits whatever the cache's unused slots hold.  No size is a limit but: rows * H and B * H at most 2^31 - 1 workgroups.
- * Workspace: d3tom_attend_cache_workspace_bytes (weighed: whether weight_out is given; 0 for arguments that the call refuses).
+ * Workspace: d3tom_attend_cache_workspace_bytes (weighed: whether weight_out is given; 0 for arguments that the call refuses), which is
+ * enough for every call on the cache with at most these rows, max_len and H, weighed or not, whatever max_q.
  * ---------------------------------------------------------------------------------------- */
 size_t d3tom_attend_cache_workspace_bytes(const d3tom_paged_cache* cache /* host */, int rows, int max_q, int max_len, int H, int weighed);
 int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_paged_cache* cache /* host */, const int32_t* q_off, int rows, int max_q,

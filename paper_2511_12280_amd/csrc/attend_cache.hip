@@ -6,6 +6,7 @@
 // What the slots got (weight_out) is formed from the joined sums behind that: p = 2^(logit - lse).
 #include "cache.hpp"
 #include "direct_load.hpp"
+#include <stdlib.h>
 
 namespace d3tom {
 
@@ -21,6 +22,7 @@ struct AttendCacheArgs {
     float *lse, *lse2;                          // natural logarithm (the caller's), base 2 (for the weights)
     float *part_o, *part_ml;                    // [rows, H, S, dh], [rows, H, S, 2]
     float* logits;                              // [rows, H, lpad], units of log 2, or none
+    int last_slot;                              // that a sample's part of the page table has a place for
     int lpad, tiles;                            // tiles: of 16 rows, of a sample and key head
     const float* weight_in;
     float* weight_out;
@@ -182,46 +184,95 @@ __device__ __forceinline__ f32x4 ac_mma(const uint4& a, const uint4& b, f32x4 c)
         return c;
     }
 }
+// Makes a load's result be there at this point.  The compiler does not count the direct loads: a register whose load it has not seen the end of in front of the loop would be
+// waited for in every turn, by a wait for everything that is on its way.
+__device__ __forceinline__ void arrived(uint4& v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
 __device__ __forceinline__ float quad_max(float v) { return quad_combine(v, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float quad_sum(float v) { return quad_combine(v, [](float a, float b) { return a + b; }); }
 #endif
 
-template <typename T, int DH>
-__global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a) {
+// A tile's logits of one block of rows, in units of log 2, to probabilities relative to the running maximum; O and the sum are scaled where that has moved.
+// It moves only where a logit is AC_SLACK above it: the probabilities are then at most 2^AC_SLACK, which costs no precision in float32 sums and none in bf16 (its
+// steps are relative), and the scaling, 4 DB multiplications, is rare behind the first tiles: with sixteen rows to a wave one of them has a new maximum in most tiles.
+// `left`: keys in front of the lane's first one that are still seen, where the tile has any that are not.
+constexpr float AC_SLACK = 6.f;
+template <int KB, int DB>
+__device__ __forceinline__ void ac_softmax(f32x4 (&st)[KB], f32x4 (&o)[DB], float& m, float& l, float scale2, bool masked, int left) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    if (masked) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st[kb][e] = kb * 16 + e < left ? st[kb][e] : -INFINITY;
+    }
+    float top = -INFINITY;                                 // (the median of two values and infinity is the larger one, without an instruction that quiets NaN first)
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = __builtin_amdgcn_fmed3f(top, st[kb][e], INFINITY);
+    top *= scale2;
+    if (__builtin_amdgcn_ballot_w64(top > m + AC_SLACK) != 0) {
+        const float mn = fmaxf(m, quad_max(top));
+        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int t = 0; t < DB; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[t][e] *= alpha;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;            // a column that has seen nothing yet: all its p are 0
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][e], scale2, -ref));
+            st[kb][e] = p;
+            sum[e] += p;
+        }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#endif
+}
+
+template <typename T, int DH, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCacheArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = AcTile<T, DH>;
     constexpr int ROWB = C::ROWB, NCHK = C::NCHK, KEYS = C::KEYS, KB = C::KB, LDB = C::LDB, RPI = C::RPI, KS = C::KS, DB = C::DB;
     extern __shared__ __attribute__((aligned(16))) char ring[];
-    __shared__ float part_m[4][16], part_l[4][16];
+    __shared__ float part_m[WAVES][16], part_l[WAVES][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-    // tiles of rows of the same keys run on one XCD, one after the other
+    // Tiles of rows of the same keys run on one XCD, one after the other; first runs first, so that the XCDs (every eighth workgroup) have samples
+    // of all lengths, and first runs, which every sample has, do not meet on some of them.
     int id = blockIdx.x;
     const int xcd = id & 7;
     id >>= 3;
     const int tile = id % a.tiles;
     int unit = (id / a.tiles) * 8 + xcd;
-    const int s = unit % a.S; unit /= a.S;
+    const int heads = a.nB * a.cache.Hkv, s = unit / heads; unit -= s * heads;
     const int kvh = unit % a.cache.Hkv, b = unit / a.cache.Hkv;
-    const int nB = a.nB;
-    if (b >= nB) return;
+    if (s >= a.S) return;
+    // Pages of this wave's blocks of 16 slots: lane i has that of block i % KB of its tile i / KB.  Requested with the sample's sizes, not behind them: what lies
+    // behind its last page is never used.
+    const int j0 = s * a.run, my_slot = j0 + ((lane / KB) * WAVES + wave) * KEYS + (lane % KB) * 16;
+    const int my_page = a.cache.page_of(b, min(my_slot, a.last_slot));
     int r0;
     const int nq = sample_rows(a, b, r0);
     const int R = nq * a.G, R0 = tile * 16;
     if (R0 >= R) return;
     const int n = a.cache.length(b, a.max_len);
     const int last = min(R0 + 15, R - 1);
-    const int j0 = s * a.run, j1 = min(row_limit(a, n, nq, last / a.G), j0 + a.run);
+    const int j1 = min(row_limit(a, n, nq, last / a.G), j0 + a.run);
     if (j0 >= j1 && s > 0) return;
     const int x = min(R0 + r, R - 1), xi = x / a.G, xh = kvh * a.G + (x - xi * a.G);          // this lane's column
     const size_t row = (size_t)(r0 + xi);
     const int limit = min(row_limit(a, n, nq, xi), j1);
     const int limit0 = min(row_limit(a, n, nq, R0 / a.G), j1);                                 // slots that all columns see
 
-    // pages of this wave's blocks of 16 slots: lane i has that of block i % KB of its tile i / KB
     const int ntile = j1 > j0 ? (j1 - j0 + KEYS - 1) / KEYS : 0;
-    const int mine = (ntile - wave + 3) / 4;                                                   // tiles wave, wave + 4, ...
-    const int my_slot = j0 + ((lane / KB) * 4 + wave) * KEYS + (lane % KB) * 16;
-    const uint32_t ids = my_slot < j1 ? a.cache.readable(a.cache.page_of(b, my_slot)) : 0u;
+    const int mine = (ntile - wave + WAVES - 1) / WAVES;                                       // tiles wave, wave + WAVES, ...
+    const uint32_t ids = a.cache.readable(my_page);
 
     uint4 qf[KS];
     {
@@ -245,7 +296,7 @@ __global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a)
     auto issue = [&](const char* base, const int (&off)[LDB], int t, uint32_t lds) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-            const int slot = j0 + (t * 4 + wave) * KEYS + kb * 16;
+            const int slot = j0 + (t * WAVES + wave) * KEYS + kb * 16;
             const uint32_t page = __builtin_amdgcn_readlane(ids, (t * KB + kb) & 63);
             const int there = t < mine ? min(max(j1 - slot, 0), 16) : 0;
             const __amdgpu_buffer_rsrc_t rs = make_uniform_rsrc(base + a.cache.row(page, slot) * row_bytes, there ? (uint32_t)(there - 1) * row_bytes + ROWB : 0u);
@@ -255,6 +306,8 @@ __global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a)
     };
     auto issue_k = [&](int t) { issue(kbase, k_off, t, ring0 + (t & 1) * C::STAGE); };
     auto issue_v = [&](int t) { issue(vbase, v_off, t, ring0 + (t & 1) * C::STAGE + C::TILE); };
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) arrived(qf[kk]);
     issue_k(0); issue_v(0); issue_k(1); issue_v(1);
 
     int k_addr[KS], v_addr[DB];
@@ -278,7 +331,7 @@ __global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a)
 
     for (int t = 0; t < mine; ++t) {
         const char* w = ring + wave * C::WAVE_LDS + (t & 1) * C::STAGE;
-        const int key0 = j0 + (t * 4 + wave) * KEYS;
+        const int key0 = j0 + (t * WAVES + wave) * KEYS;
         wait_loads<3 * C::LD>();                           // K of this tile is there
         f32x4 st[KB];
 #pragma unroll
@@ -289,46 +342,12 @@ __global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a)
         }
         wait_lds();
         issue_k(t + 2);
-        float top = -INFINITY;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) st[kb][e] *= a.scale2;
-        if (key0 + KEYS > limit0) {
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) st[kb][e] = key0 + kb * 16 + 4 * g + e < limit ? st[kb][e] : -INFINITY;
-        }
         if (kept && real) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
-                if (key0 + kb * 16 < j1) *reinterpret_cast<f32x4*>(kept + key0 + kb * 16 + 4 * g) = st[kb];
+                if (key0 + kb * 16 < j1) *reinterpret_cast<f32x4*>(kept + key0 + kb * 16 + 4 * g) = f32x4{st[kb][0] * a.scale2, st[kb][1] * a.scale2, st[kb][2] * a.scale2, st[kb][3] * a.scale2};
         }
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) top = fmaxf(top, st[kb][e]);
-        top = quad_max(top);
-        if (__builtin_amdgcn_ballot_w64(top > m) != 0) {
-            const float mn = fmaxf(m, top);
-            const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-            m = mn;
-            l *= alpha;
-#pragma unroll
-            for (int t2 = 0; t2 < DB; ++t2)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[t2][e] *= alpha;
-        }
-        const float ref = m == -INFINITY ? 0.f : m;        // a column that has seen nothing yet: all its p are 0
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float p = __builtin_amdgcn_exp2f(st[kb][e] - ref);
-                st[kb][e] = p;
-                l += p;
-            }
+        ac_softmax<KB, DB>(st, o, m, l, a.scale2, key0 + KEYS > limit0, limit - key0 - 4 * g);
         wait_loads<3 * C::LD>();                           // V of this tile
         if constexpr (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) ac_short4* tr_ptr;
@@ -358,7 +377,7 @@ __global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a)
         issue_v(t + 2);
     }
     wait_loads_and_barrier<0>();                           // nothing is on its way into the rings any more
-    // the four waves' parts, rows of queries
+    // the waves' parts, rows of queries
     float* part = reinterpret_cast<float*>(ring);
     l = quad_sum(l);
     float* to = part + (wave * 16 + r) * C::PITCH + 4 * g;
@@ -366,28 +385,28 @@ __global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a)
     for (int t = 0; t < DB; ++t) *reinterpret_cast<f32x4*>(to + t * 16) = o[t];
     if (g == 0) { part_m[wave][r] = m; part_l[wave][r] = l; }
     __syncthreads();
-    // sixteen threads to a row
-    const int y = tid >> 4, Y = R0 + y;
+    // four threads of every wave to a row
+    constexpr int TPR = 4 * WAVES, CH = DH / TPR;
+    const int y = tid / TPR, Y = R0 + y;
     if (Y >= R) return;
     const int yi = Y / a.G, yh = kvh * a.G + (Y - yi * a.G);
     float mt = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mt = fmaxf(mt, part_m[w][y]);
-    float f[4], z = 0.f;
+    for (int w = 0; w < WAVES; ++w) mt = fmaxf(mt, part_m[w][y]);
+    float f[WAVES], z = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         f[w] = part_m[w][y] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part_m[w][y] - mt);
         z += part_l[w][y] * f[w];
     }
     const size_t at = ((size_t)(r0 + yi) * a.H + yh) * a.S + s;
     const float inv = a.S > 1 ? 1.f : z > 0.f ? 1.0f / z : 0.f;
-    constexpr int CH = DH / 16;
-    const int c0 = (tid & 15) * CH;
+    const int c0 = (tid % TPR) * CH;
     float acc[CH];
 #pragma unroll
     for (int e = 0; e < CH; ++e) acc[e] = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
+    for (int w = 0; w < WAVES; ++w)
 #pragma unroll
         for (int e = 0; e < CH; ++e) acc[e] = __builtin_fmaf(part[(w * 16 + y) * C::PITCH + c0 + e], f[w], acc[e]);
 #pragma unroll
@@ -395,7 +414,7 @@ __global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a)
     if (a.S > 1) {
 #pragma unroll
         for (int e = 0; e < CH; e += 4) *reinterpret_cast<f32x4*>(a.part_o + at * DH + c0 + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-        if ((tid & 15) == 0) { a.part_ml[at * 2] = mt; a.part_ml[at * 2 + 1] = z; }
+        if (c0 == 0) { a.part_ml[at * 2] = mt; a.part_ml[at * 2 + 1] = z; }
     } else {
         T* out = static_cast<T*>(a.o) + at * DH + c0;
         if constexpr (sizeof(T) == 2) store_bf16<CH>(out, acc);
@@ -403,7 +422,7 @@ __global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a)
 #pragma unroll
             for (int e = 0; e < CH; e += 4) *reinterpret_cast<f32x4*>(out + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
         }
-        if ((tid & 15) == 0) {
+        if (c0 == 0) {
             const float l2 = z > 0.f ? mt + log2f(z) : -INFINITY;
             if (a.lse) a.lse[at] = l2 * 0.6931471805599453f;
             if (a.lse2) a.lse2[at] = l2;
@@ -412,41 +431,45 @@ __global__ __launch_bounds__(256, 1) void attend_cache_kernel(AttendCacheArgs a)
 #endif
 }
 
-
-// More than 16 rows to a key head: the waves share the tiles and have QB blocks of 16 rows each, so that a key's row is read from LDS four times
-// and from memory once for 64 QB rows.  Tiles of 16 KB of K and of V, of which every wave loads a quarter, in a ring of two stages; two
-// workgroups to a compute unit, so that one's exponentials run beside the other's matrix instructions.
+// More than 16 rows to a key head: eight waves share the tiles.  Wave (kg, rg) has QB blocks of 16 rows (of four such groups rg) and half of every tile's keys, so that a
+// key's row is read from LDS four times and from memory once for 64 QB rows, and two waves of a SIMD alternate between matrix instructions and
+// exponentials.  Tiles of 16 KB of K and of V, of which every wave loads an eighth, in a ring of four stages; one barrier a tile: behind it this tile is there for everybody, and
+// everybody is done with the last but one, whose place is loaded again.  At the end the two waves of the same rows exchange halves of the channels.
 template <typename T, int DH> struct AcShared {
     using C = AcTile<T, DH>;
-    static constexpr int TILE = 16384, KEYS = TILE / C::ROWB, KB = KEYS / 16, LD = 4, STAGE = 2 * TILE, LDS = 2 * STAGE;
+    static constexpr int TILE = 16384, KEYS = TILE / C::ROWB, KB = KEYS / 16, LD = 2, STAGE = 2 * TILE, STAGES = 4, LDS = STAGES * STAGE;
+    static constexpr int KW = KB / 2;                  // blocks of 16 keys of a wave
     static constexpr int PAGES = 256;                  // blocks of 16 slots of a run whose pages lie in LDS
 };
 template <typename T, int DH, int QB>
-__global__ __launch_bounds__(256, 2) void attend_cache_rows_kernel(AttendCacheArgs a) {
+__global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = AcTile<T, DH>;
     using W = AcShared<T, DH>;
-    constexpr int ROWB = C::ROWB, NCHK = C::NCHK, KEYS = W::KEYS, KB = W::KB, LD = W::LD, RPI = C::RPI, KS = C::KS, DB = C::DB;
+    constexpr int ROWB = C::ROWB, NCHK = C::NCHK, KEYS = W::KEYS, KB = W::KB, KW = W::KW, LD = W::LD, RPI = C::RPI, KS = C::KS, DB = C::DB;
     extern __shared__ __attribute__((aligned(16))) char ring[];
     __shared__ uint32_t pages[W::PAGES];
+    __shared__ float other_m[2][4][QB * 16], other_l[2][4][QB * 16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    const int kg = wave >> 2, rg = wave & 3;
     int id = blockIdx.x;
     const int xcd = id & 7;
     id >>= 3;
     const int tile = id % a.tiles;
     int unit = (id / a.tiles) * 8 + xcd;
-    const int s = unit % a.S; unit /= a.S;
+    const int heads = a.nB * a.cache.Hkv, s = unit / heads; unit -= s * heads;
     const int kvh = unit % a.cache.Hkv, b = unit / a.cache.Hkv;
-    if (b >= a.nB) return;
+    if (s >= a.S) return;
+    const int j0 = s * a.run, my_page = a.cache.page_of(b, min(j0 + (tid & (W::PAGES - 1)) * 16, a.last_slot));         // (see above)
     int r0;
     const int nq = sample_rows(a, b, r0);
     constexpr int ROWS = 64 * QB;
     const int R = nq * a.G, R0 = tile * ROWS;
     if (R0 >= R) return;
     const int n = a.cache.length(b, a.max_len);
-    const int j0 = s * a.run, j1 = min(row_limit(a, n, nq, (min(R0 + ROWS, R) - 1) / a.G), j0 + a.run);
+    const int j1 = min(row_limit(a, n, nq, (min(R0 + ROWS, R) - 1) / a.G), j0 + a.run);
     if (j0 >= j1 && s > 0) return;
-    const int W0 = R0 + wave * 16 * QB;                // this wave's first row
+    const int W0 = R0 + rg * 16 * QB;                  // this wave's first row
     const bool works = W0 < R;
     size_t row[QB];
     int xh[QB], limit[QB];
@@ -459,10 +482,7 @@ __global__ __launch_bounds__(256, 2) void attend_cache_rows_kernel(AttendCacheAr
     }
     const int limit0 = min(row_limit(a, n, nq, min(W0, R - 1) / a.G), j1);
     const int ntile = j1 > j0 ? (j1 - j0 + KEYS - 1) / KEYS : 0;
-    {
-        const int slot = j0 + tid * 16;
-        pages[tid] = slot < j1 ? a.cache.readable(a.cache.page_of(b, slot)) : 0u;
-    }
+    if (tid < W::PAGES) pages[tid] = a.cache.readable(my_page);
     uint4 qf[QB][KS];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
@@ -484,7 +504,7 @@ __global__ __launch_bounds__(256, 2) void attend_cache_rows_kernel(AttendCacheAr
     }
     // this wave's loads of tile t; `ids`: lane i has the page of the tile's block i
     auto issue = [&](int t, uint32_t ids) {
-        const uint32_t lds = ring0 + (t & 1) * W::STAGE + wave * LD * 1024;
+        const uint32_t lds = ring0 + (t & (W::STAGES - 1)) * W::STAGE + wave * LD * 1024;
 #pragma unroll
         for (int i = 0; i < LD; ++i) {
             const int kb = (wave * LD + i) * RPI / 16, slot = j0 + t * KEYS + kb * 16;
@@ -498,19 +518,24 @@ __global__ __launch_bounds__(256, 2) void attend_cache_rows_kernel(AttendCacheAr
     };
     auto pages_of = [&](int t) { return pages[min(t * KB + (lane & (KB - 1)), W::PAGES - 1)]; };
     __syncthreads();
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) arrived(qf[qb][kk]);
     issue(0, pages_of(0));
     issue(1, pages_of(1));
 
     int k_addr[KS], v_addr[DB];
+    const int half = kg * KW * 16 * ROWB;              // this wave's keys of a tile
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk) k_addr[kk] = r * ROWB + (((kk * 4 + g) ^ C::k_turn(r)) << 4);
+    for (int kk = 0; kk < KS; ++kk) k_addr[kk] = half + r * ROWB + (((kk * 4 + g) ^ C::k_turn(r)) << 4);
 #pragma unroll
     for (int t = 0; t < DB; ++t) {
         if constexpr (sizeof(T) == 2) {
             const int vr = 4 * g + (r >> 2), chunk = t * 2 + ((r & 3) >> 1);
-            v_addr[t] = W::TILE + vr * ROWB + ((chunk ^ C::v_turn(vr)) << 4) + (r & 1) * 8;
+            v_addr[t] = W::TILE + half + vr * ROWB + ((chunk ^ C::v_turn(vr)) << 4) + (r & 1) * 8;
         } else {
-            v_addr[t] = W::TILE + 4 * g * ROWB + (((t * 4 + (r >> 2)) ^ C::v_turn(4 * g)) << 4) + (r & 3) * 4;
+            v_addr[t] = W::TILE + half + 4 * g * ROWB + (((t * 4 + (r >> 2)) ^ C::v_turn(4 * g)) << 4) + (r & 3) * 4;
         }
     }
     f32x4 o[QB][DB];
@@ -521,179 +546,365 @@ __global__ __launch_bounds__(256, 2) void attend_cache_rows_kernel(AttendCacheAr
 #pragma unroll
         for (int t = 0; t < DB; ++t) o[qb][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    for (int t = 0; t < ntile; ++t) {
-        wait_loads_and_barrier<2 * LD>();              // everybody's part of this tile is there
-        const char* w = ring + (t & 1) * W::STAGE;
-        const int key0 = j0 + t * KEYS;
-        const uint32_t ids = pages_of(t + 2);
-        if (works) {
-            f32x4 st[QB][KB];
+    f32x4 st[QB][KW];
+    uint4 kf[KW][KS];
+    constexpr int VN = sizeof(T) == 2 ? KW / 2 : KW;
+    f32x4 vf[VN][DB];                                  // bf16: the 8 keys of a lane; float32: its 4
+    auto read_k = [&](int t) {
+        const char* w = ring + (t & (W::STAGES - 1)) * W::STAGE;
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
+        for (int kb = 0; kb < KW; ++kb)
 #pragma unroll
-                for (int qb = 0; qb < QB; ++qb) st[qb][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int kk = 0; kk < KS; ++kk) kf[kb][kk] = *reinterpret_cast<const uint4*>(w + k_addr[kk] + kb * 16 * ROWB);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto read_v = [&](int t) {
+        const char* w = ring + (t & (W::STAGES - 1)) * W::STAGE;
 #pragma unroll
-                for (int kk = 0; kk < KS; ++kk) {
-                    const uint4 kf = *reinterpret_cast<const uint4*>(w + k_addr[kk] + kb * 16 * ROWB);
+        for (int i = 0; i < VN; ++i)
 #pragma unroll
-                    for (int qb = 0; qb < QB; ++qb) st[qb][kb] = ac_mma<T>(kf, qf[qb][kk], st[qb][kb]);
+            for (int t2 = 0; t2 < DB; ++t2) {
+                if constexpr (sizeof(T) == 2) {
+                    typedef __attribute__((address_space(3))) ac_short4* tr_ptr;
+                    const char* p = w + v_addr[t2] + i * 32 * ROWB;
+                    const ac_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + 16 * ROWB));
+                    vf[i][t2] = __builtin_bit_cast(f32x4, ac_short8(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) vf[i][t2][e] = *reinterpret_cast<const float*>(w + v_addr[t2] + (i * 16 + e) * ROWB);
                 }
             }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto scores = [&]() {                              // S = K Q^T
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
+        for (int kb = 0; kb < KW; ++kb)
 #pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
+            for (int qb = 0; qb < QB; ++qb) st[qb][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) st[qb][kb][e] *= a.scale2;
-                if (key0 + KEYS > limit0) {
+        for (int kk = 0; kk < KS; ++kk)
 #pragma unroll
-                    for (int kb = 0; kb < KB; ++kb)
+            for (int kb = 0; kb < KW; ++kb)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) st[qb][kb][e] = key0 + kb * 16 + 4 * g + e < limit[qb] ? st[qb][kb][e] : -INFINITY;
-                }
-                float top = -INFINITY;
+                for (int qb = 0; qb < QB; ++qb) st[qb][kb] = ac_mma<T>(kf[kb][kk], qf[qb][kk], st[qb][kb]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto softmax = [&](int t) {
+        const int key0 = j0 + t * KEYS + kg * KW * 16;
 #pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
+        for (int qb = 0; qb < QB; ++qb) ac_softmax<KW, DB>(st[qb], o[qb], m[qb], l[qb], a.scale2, key0 + KW * 16 > limit0, limit[qb] - key0 - 4 * g);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto values = [&]() {                              // O += V P
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) top = fmaxf(top, st[qb][kb][e]);
-                top = quad_max(top);
-                if (__builtin_amdgcn_ballot_w64(top > m[qb]) != 0) {
-                    const float mn = fmaxf(m[qb], top);
-                    const float alpha = m[qb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[qb] - mn);
-                    m[qb] = mn;
-                    l[qb] *= alpha;
+            for (int kp = 0; kp < VN; ++kp) {
+                bf16x8 pf[QB];
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { pf[qb][e] = (__bf16)st[qb][2 * kp][e]; pf[qb][4 + e] = (__bf16)st[qb][2 * kp + 1][e]; }
+#pragma unroll
+                for (int t2 = 0; t2 < DB; ++t2)
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb) o[qb][t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[kp][t2]), pf[qb], o[qb][t2], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < VN; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
                     for (int t2 = 0; t2 < DB; ++t2)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[qb][t2][e] *= alpha;
-                }
-                const float ref = m[qb] == -INFINITY ? 0.f : m[qb];
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float p = __builtin_amdgcn_exp2f(st[qb][kb][e] - ref);
-                        st[qb][kb][e] = p;
-                        l[qb] += p;
-                    }
-            }
-            if constexpr (sizeof(T) == 2) {
-                typedef __attribute__((address_space(3))) ac_short4* tr_ptr;
-#pragma unroll
-                for (int kp = 0; kp < KB / 2; ++kp) {
-                    bf16x8 pf[QB];
-#pragma unroll
-                    for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) { pf[qb][e] = (__bf16)st[qb][2 * kp][e]; pf[qb][4 + e] = (__bf16)st[qb][2 * kp + 1][e]; }
-#pragma unroll
-                    for (int t2 = 0; t2 < DB; ++t2) {
-                        const char* p = w + v_addr[t2] + kp * 32 * ROWB;
-                        const ac_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + 16 * ROWB));
-                        const ac_short8 v8 = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-                        for (int qb = 0; qb < QB; ++qb) o[qb][t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v8), pf[qb], o[qb][t2], 0, 0, 0);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                    for (int t2 = 0; t2 < DB; ++t2)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float v = *reinterpret_cast<const float*>(w + v_addr[t2] + (kb * 16 + e) * ROWB);
-#pragma unroll
-                            for (int qb = 0; qb < QB; ++qb) o[qb][t2] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, st[qb][kb][e], o[qb][t2], 0, 0, 0);
-                        }
-            }
+                        for (int qb = 0; qb < QB; ++qb) o[qb][t2] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[kb][t2][e], st[qb][kb][e], o[qb][t2], 0, 0, 0);
         }
-        wait_lds();
-        phase_barrier();                               // everybody has read this tile
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // Waves of half 1 are half a tile behind: they meet the others for the next tile between their two products, so that a SIMD's two waves want its vector
+    // and matrix units in turn.  (The tile before is then still read: two are on their way.)  Every wave comes to every barrier.
+    uint32_t ids = pages_of(2);
+    auto meet = [&](int t) {                           // tile t is there, tile t - 2 is done with
+        wait_loads_and_barrier<2 * LD>();
         issue(t + 2, ids);
+        ids = pages_of(t + 3);
+    };
+    if (ntile > 0) meet(0);
+    for (int t = 0; t < ntile; ++t) {
+        if (kg == 0 && t > 0) meet(t);
+        if (works) {
+            read_k(t);
+            scores();
+        }
+        if (kg == 1 && t + 1 < ntile) meet(t + 1);
+        if (works) {
+            read_v(t);
+            softmax(t);
+            values();
+        }
     }
-    wait_loads<0>();                                   // nothing is on its way into LDS when the workgroup ends
+    wait_loads_and_barrier<0>();                       // nothing is on its way into LDS any more, and nobody reads the ring
+    // wave kg keeps the channels of half kg and gives the others away
+    f32x4* swap = reinterpret_cast<f32x4*>(ring);
+    constexpr int HD = DB / 2;
+    if (works) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            l[qb] = quad_sum(l[qb]);
+            if (g == 0) { other_m[kg][rg][qb * 16 + r] = m[qb]; other_l[kg][rg][qb * 16 + r] = l[qb]; }
+#pragma unroll
+            for (int t = 0; t < HD; ++t) swap[(((rg * QB + qb) * 2 + kg) * HD + t) * 64 + lane] = kg ? o[qb][t] : o[qb][HD + t];
+        }
+    }
+    __syncthreads();
     if (!works) return;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         if (W0 + qb * 16 + r >= R) continue;
-        const float z = quad_sum(l[qb]);
+        const float m2 = other_m[kg ^ 1][rg][qb * 16 + r], l2 = other_l[kg ^ 1][rg][qb * 16 + r];
+        const float mt = fmaxf(m[qb], m2);
+        const float f1 = m[qb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[qb] - mt), f2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m2 - mt);
+        // (in the same order in both waves)
+        const float z = kg ? __builtin_fmaf(l2, f2, l[qb] * f1) : __builtin_fmaf(l[qb], f1, l2 * f2);
         const size_t at = (row[qb] * a.H + xh[qb]) * a.S + s;
         const float inv = a.S > 1 ? 1.f : z > 0.f ? 1.0f / z : 0.f;
 #pragma unroll
-        for (int t = 0; t < DB; ++t) {
-            const f32x4 v = {o[qb][t][0] * inv, o[qb][t][1] * inv, o[qb][t][2] * inv, o[qb][t][3] * inv};
-            const size_t to = at * DH + t * 16 + 4 * g;
-            if (a.S > 1) *reinterpret_cast<f32x4*>(a.part_o + to) = v;
-            else if constexpr (sizeof(T) == 2) { const float w4[4] = {v[0], v[1], v[2], v[3]}; store_bf16<4>(static_cast<T*>(a.o) + to, w4); }
-            else *reinterpret_cast<f32x4*>(static_cast<T*>(a.o) + to) = v;
+        for (int t = 0; t < HD; ++t) {
+            const f32x4 x = kg ? o[qb][HD + t] : o[qb][t], y = swap[(((rg * QB + qb) * 2 + (kg ^ 1)) * HD + t) * 64 + lane];
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(x[e], f1, y[e] * f2) * inv;
+            const size_t to = at * DH + (kg * HD + t) * 16 + 4 * g;
+            if (a.S > 1) *reinterpret_cast<f32x4*>(a.part_o + to) = f32x4{v[0], v[1], v[2], v[3]};
+            else if constexpr (sizeof(T) == 2) store_bf16<4>(static_cast<T*>(a.o) + to, v);
+            else *reinterpret_cast<f32x4*>(static_cast<T*>(a.o) + to) = f32x4{v[0], v[1], v[2], v[3]};
         }
-        if (g == 0) {
-            if (a.S > 1) { a.part_ml[at * 2] = m[qb]; a.part_ml[at * 2 + 1] = z; }
+        if (g == 0 && kg == 0) {
+            if (a.S > 1) { a.part_ml[at * 2] = mt; a.part_ml[at * 2 + 1] = z; }
             else {
-                const float l2 = z > 0.f ? m[qb] + log2f(z) : -INFINITY;
-                if (a.lse) a.lse[at] = l2 * 0.6931471805599453f;
-                if (a.lse2) a.lse2[at] = l2;
+                const float lt = z > 0.f ? mt + log2f(z) : -INFINITY;
+                if (a.lse) a.lse[at] = lt * 0.6931471805599453f;
+                if (a.lse2) a.lse2[at] = lt;
             }
         }
     }
 #endif
 }
 
+// The runs of the rows joined: dh / 4 threads to a row and head, and `groups` such groups of threads that have every groups-th run, JW_UNROLL of them requested
+// together, so that few runs are one trip to memory; the groups meet in LDS.
+constexpr int JW_UNROLL = 4;
+__device__ __forceinline__ int runs_of(const AttendCacheArgs& a, int limit) { return max(1, (limit + a.run - 1) / a.run); }
+
+template <int NT> struct JoinLds { f32x4 t[NT]; float m[NT / 4], z[NT / 4]; };
+template <typename T, int NT>
+__device__ __forceinline__ void join_rows(const AttendCacheArgs& a, int b, int block, int groups, JoinLds<NT>& lds) {
+    const int tid = threadIdx.x, dh = a.cache.dh;
+    int r0;
+    const int nq = sample_rows(a, b, r0);
+    const int n = a.cache.length(b, a.max_len);
+    const int tpr = dh >> 2, per = NT / tpr / groups, y = tid / tpr, c = tid - y * tpr;
+    const int which = y / groups, g = y - which * groups, item = block * per + which;
+    const bool there = which < per && item < nq * a.H;
+    const size_t at = (size_t)r0 * a.H + item;
+    float m = -INFINITY, z = 0.f;
+    f32x4 t = {0.f, 0.f, 0.f, 0.f};
+    if (there) {
+        const int S = runs_of(a, row_limit(a, n, nq, item / a.H));
+        const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + at * a.S;
+        const f32x4* part = reinterpret_cast<const f32x4*>(a.part_o + at * a.S * dh) + c;
+        for (int s = g; s < S; s += groups * JW_UNROLL) {
+            float2 v[JW_UNROLL];
+            f32x4 p[JW_UNROLL];
+#pragma unroll
+            for (int u = 0; u < JW_UNROLL; ++u) {
+                const int su = min(s + u * groups, S - 1);
+                v[u] = ml[su];
+                p[u] = part[(size_t)su * tpr];
+            }
+            float mn = m;
+#pragma unroll
+            for (int u = 0; u < JW_UNROLL; ++u) mn = fmaxf(mn, v[u].x);             // (a run that comes twice does not change it)
+            const float ref = mn == -INFINITY ? 0.f : mn, f0 = exp2f(m - ref);
+            m = mn;
+            z *= f0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] *= f0;
+#pragma unroll
+            for (int u = 0; u < JW_UNROLL; ++u) {
+                const float f = s + u * groups < S ? exp2f(v[u].x - ref) : 0.f;
+                z = __builtin_fmaf(v[u].y, f, z);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] = __builtin_fmaf(p[u][e], f, t[e]);
+            }
+        }
+    }
+    if (groups > 1) {
+        lds.t[tid] = t;
+        if (c == 0 && y < NT / 4) { lds.m[y] = m; lds.z[y] = z; }
+        __syncthreads();
+        if (there && g == 0) {
+            float mt = m;
+            for (int i = 1; i < groups; ++i) mt = fmaxf(mt, lds.m[y + i]);
+            const float ref = mt == -INFINITY ? 0.f : mt, f0 = exp2f(m - ref);
+            z *= f0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] *= f0;
+            for (int i = 1; i < groups; ++i) {
+                const float f = exp2f(lds.m[y + i] - ref);
+                const f32x4 p = lds.t[tid + i * tpr];
+                z = __builtin_fmaf(lds.z[y + i], f, z);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] = __builtin_fmaf(p[e], f, t[e]);
+            }
+            m = mt;
+        }
+    }
+    if (!there || g != 0) return;
+    const float inv = z > 0.f ? 1.0f / z : 0.f;
+    T* o = static_cast<T*>(a.o) + at * dh + c * 4;
+    const float w[4] = {t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv};
+    if constexpr (sizeof(T) == 2) store_bf16<4>(o, w);
+    else *reinterpret_cast<f32x4*>(o) = f32x4{w[0], w[1], w[2], w[3]};
+    if (c == 0) {
+        const float l2 = z > 0.f ? m + log2f(z) : -INFINITY;
+        if (a.lse) a.lse[at] = l2 * 0.6931471805599453f;
+        if (a.lse2) a.lse2[at] = l2;
+    }
+}
+
+// log-sum-exp (units of log 2) of `cnt` rows and heads from item c0 on, into LDS: from their runs, by TPI threads to a row and head, or as it stands in a.lse2
+template <int NT, int TPI>
+__device__ __forceinline__ void runs_lse2(const AttendCacheArgs& a, int r0, int nq, int n, int c0, int cnt, float* lse2) {
+    constexpr int AT_ONCE = 8;                         // runs requested together
+    const int sub = threadIdx.x % TPI;
+    for (int u0 = 0; u0 < cnt; u0 += NT / TPI) {       // (all lanes together: they exchange what they have)
+        const int u = u0 + threadIdx.x / TPI, uc = min(u, cnt - 1), S = runs_of(a, row_limit(a, n, nq, (c0 + uc) / a.H));
+        const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + ((size_t)r0 * a.H + c0 + uc) * a.S;
+        float m = -INFINITY, z = 0.f;
+        for (int s = sub; s < S; s += TPI * AT_ONCE) {
+            float2 v[AT_ONCE];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) v[i] = ml[min(s + i * TPI, S - 1)];
+            float mn = m;
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) mn = fmaxf(mn, v[i].x);
+            const float ref = mn == -INFINITY ? 0.f : mn;
+            z *= __builtin_amdgcn_exp2f(m - ref);
+            m = mn;
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) z += s + i * TPI < S ? v[i].y * __builtin_amdgcn_exp2f(v[i].x - ref) : 0.f;
+        }
+#pragma unroll
+        for (int o = 1; o < TPI; o <<= 1) lse2_combine_fast(m, z, __shfl_xor(m, o), __shfl_xor(z, o));
+        if (sub == 0 && u < cnt) lse2[u] = m + log2f(z);
+    }
+}
+template <int NT>
+__device__ __forceinline__ void rows_lse2(const AttendCacheArgs& a, int r0, int nq, int n, int c0, int cnt, float* lse2) {
+    if (a.S == 1) {
+        for (int u = threadIdx.x; u < cnt; u += NT) lse2[u] = a.lse2[(size_t)r0 * a.H + c0 + u];
+    } else if (cnt * 8 <= NT) {
+        runs_lse2<NT, 8>(a, r0, nq, n, c0, cnt, lse2);
+    } else {
+        runs_lse2<NT, 1>(a, r0, nq, n, c0, cnt, lse2);
+    }
+}
+
 // What the slots got where the logits are not kept: they are formed again, K Q^T once more (the keys' rows a third time through memory is less than
 // 4 bytes a logit there and back).  A workgroup has a tile of a sample's slots and goes over all heads and rows, wave w over key heads w, w + 8, ...
-// (or parts of a head's rows where there are fewer); the keys of a head lie in its registers, the queries come from the caches.
+// (or parts of a head's rows where there are fewer); the keys of a head lie in its registers, the queries come from the caches, one block of 16 rows ahead.  Bound by vector
+// instructions: an fma, an exp2 and an addition a logit.  (The rows' lse come from the joining launch in front: formed by every workgroup for itself in one launch with
+// the joining, four samples of 128 rows to a key head took 27 us instead of 21.)
 constexpr int CW_WAVES = 8;
+constexpr int cw_blocks(int ks) { return ks > 4 ? 2 : 4; }            // of 16 keys, in registers
 template <typename T, int DH>
 __global__ __launch_bounds__(CW_WAVES * 64) void cache_weigh_kernel(AttendCacheArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = AcTile<T, DH>;
-    constexpr int KS = C::KS, KB = C::KS > 4 ? 2 : 4, KEYS = KB * 16;
+    constexpr int KS = C::KS, KB = cw_blocks(KS), KEYS = KB * 16;
     __shared__ float sums[CW_WAVES][KEYS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-    const int b = blockIdx.y;
-    const int n = a.cache.length(b, a.max_len), key0 = blockIdx.x * KEYS;
+    const int b = blockIdx.y, key0 = blockIdx.x * KEYS;
+    int page[KB];                                       // of the tile's blocks, requested with the sample's sizes
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) page[kb] = a.cache.page_of(b, min(key0 + kb * 16, a.last_slot));
+    const int n = a.cache.length(b, a.max_len);
     if (key0 >= n) return;
     int r0;
     const int nq = sample_rows(a, b, r0), R = nq * a.G;
+    const int jt = key0 + tid;
+    const size_t to = (size_t)b * a.weight_stride + jt;
+    const float before = tid < KEYS && jt < n && a.weight_in ? a.weight_in[to] : 0.f;
     const size_t row_bytes = a.cache.row_elems() * sizeof(T);
     const char* kp[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-        const int j = min(key0 + kb * 16 + r, n - 1);
-        kp[kb] = static_cast<const char*>(a.k_pages) + a.cache.row(a.cache.readable(a.cache.page_of(b, j)), j) * row_bytes + g * 16;
+        const int at = min(key0 + kb * 16, (n - 1) & ~15), j = min(at + r, n - 1);         // blocks behind the last one: that one again
+        const int p = at == key0 + kb * 16 ? page[kb] : a.cache.page_of(b, at);
+        kp[kb] = static_cast<const char*>(a.k_pages) + a.cache.row(a.cache.readable(p), j) * row_bytes + g * 16;
     }
     f32x4 acc[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) acc[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int parts = a.cache.Hkv >= CW_WAVES ? 1 : (CW_WAVES + a.cache.Hkv - 1) / a.cache.Hkv;
-    for (int it = wave; it < a.cache.Hkv * parts; it += CW_WAVES) {
-        const int kvh = it / parts, part = it - kvh * parts;
-        if (part * 16 >= R) continue;
-        uint4 kf[KB][KS];
+    const int step_i = parts * 16 / a.G, step_x = parts * 16 - step_i * a.G;               // rows and heads from one block to the next
+    uint4 kf[KB][KS];
+    auto keys = [&](int kvh) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int kk = 0; kk < KS; ++kk) kf[kb][kk] = *reinterpret_cast<const uint4*>(kp[kb] + (size_t)kvh * C::ROWB + kk * 64);
-        for (int x0 = part * 16; x0 < R; x0 += parts * 16) {
-            const int x = min(x0 + r, R - 1), xi = x / a.G, xh = kvh * a.G + (x - xi * a.G);
-            const size_t row = (size_t)(r0 + xi);
-            const char* q = static_cast<const char*>(a.q) + (row * a.q_stride + (size_t)xh * DH) * sizeof(T) + g * 16;
-            const float lse2 = a.lse2[row * a.H + xh];
-            const int limit = x0 + r < R ? row_limit(a, n, nq, xi) : 0;
-            uint4 qf[KS];
+    };
+    for (int it = wave; it < a.cache.Hkv * parts; it += CW_WAVES) {
+        const int kvh = it / parts, part = it - kvh * parts;
+        if (part * 16 >= R) continue;
+        keys(kvh);
+        // this lane's row and head of the block that is requested next
+        int xi = (part * 16 + r) / a.G, xr = part * 16 + r - xi * a.G;
+        uint4 qf[KS];
+        float lse2;
+        int limit;
+        auto request = [&]() {
+            const int i = min(xi, nq - 1);
+            lse2 = a.lse2[(size_t)(r0 + i) * a.H + kvh * a.G + xr];
+            limit = xi < nq ? row_limit(a, n, nq, xi) : 0;
+            const char* q = static_cast<const char*>(a.q) + ((size_t)(r0 + i) * a.q_stride + (size_t)(kvh * a.G + xr) * DH) * sizeof(T) + g * 16;
 #pragma unroll
             for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const uint4*>(q + kk * 64);
+            xi += step_i;
+            xr += step_x;
+            if (xr >= a.G) { xr -= a.G; ++xi; }
+        };
+        request();
+        // (two different texts, for the compiler: the requests in front of the loop and in it would otherwise become one, at the loop's top, behind the products)
+        asm volatile("; first rows" ::: "memory");
+        for (int x0 = part * 16; x0 < R; x0 += parts * 16) {
+            const float ref = lse2;
+            const int seen = limit - key0 - 4 * g;
+            const bool masked = __builtin_amdgcn_ballot_w64(limit < key0 + KEYS) != 0;
+            f32x4 st[KB];
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                f32x4 st = {0.f, 0.f, 0.f, 0.f};
+            for (int kb = 0; kb < KB; ++kb) st[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int kk = 0; kk < KS; ++kk) st = ac_mma<T>(kf[kb][kk], qf[kk], st);
+            for (int kk = 0; kk < KS; ++kk)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(st[e] * a.scale2 - lse2);
-                    acc[kb][e] += key0 + kb * 16 + 4 * g + e < limit ? p : 0.f;
-                }
+                for (int kb = 0; kb < KB; ++kb) st[kb] = ac_mma<T>(kf[kb][kk], qf[kk], st[kb]);
+            request();
+            asm volatile("; next rows" ::: "memory");
+            if (masked) {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][e], a.scale2, -ref));
+                        acc[kb][e] += kb * 16 + e < seen ? p : 0.f;
+                    }
+            } else {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[kb][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][e], a.scale2, -ref));
             }
         }
     }
@@ -705,145 +916,63 @@ __global__ __launch_bounds__(CW_WAVES * 64) void cache_weigh_kernel(AttendCacheA
             if (r == 0) sums[wave][kb * 16 + 4 * g + e] = v;
         }
     __syncthreads();
-    const int j = key0 + tid;
-    if (tid < KEYS && j < n) {
+    if (tid < KEYS && jt < n) {
         float total = 0.f;
 #pragma unroll
         for (int w = 0; w < CW_WAVES; ++w) total += sums[w][tid];
-        const size_t at = (size_t)b * a.weight_stride + j;
-        a.weight_out[at] = (a.weight_in ? a.weight_in[at] : 0.f) + total / (float)a.H;
+        a.weight_out[to] = before + total / (float)a.H;
     }
 #endif
 }
 
-// The runs of the rows joined: dh / 4 threads to a row and head, and `groups` such groups of threads that have every groups-th run, so that few
-// runs are one trip to memory; they meet in LDS.  And, where the logits were kept, what the slots got: one thread to a slot, over all rows and heads of the sample,
-// p = 2^(logit - lse), with the rows' lse formed from the runs' sums by every workgroup for itself, eight threads to a row (a launch of its own for
-// that would cost more).
+// Joins, and what the slots got where the logits were kept: p = 2^(logit - lse), with the rows' lse formed from the runs' sums by every workgroup for itself (a launch
+// of its own for that would cost more).
 constexpr int JW_ROWS = 1024;                  // rows and heads whose lse a workgroup holds at a time
-constexpr int JW_UNROLL = 4;                   // runs requested at once
-
-__device__ __forceinline__ int runs_of(const AttendCacheArgs& a, int limit) { return max(1, (limit + a.run - 1) / a.run); }
-
+constexpr int JW_BATCH = 8;                    // rows of logits requested at once
 template <typename T>
 __global__ __launch_bounds__(256) void attend_cache_join_kernel(AttendCacheArgs a, int join_wgs, int groups) {
     __shared__ float lse2[JW_ROWS];
-    __shared__ float gm[64], gz[64];
-    __shared__ __attribute__((aligned(16))) f32x4 gt[256];
-    const int tid = threadIdx.x, b = blockIdx.y, dh = a.cache.dh;
+    __shared__ __attribute__((aligned(16))) JoinLds<256> lds;
+    const int tid = threadIdx.x, b = blockIdx.y;
+    if ((int)blockIdx.x < join_wgs) {
+        join_rows<T, 256>(a, b, blockIdx.x, groups, lds);
+        return;
+    }
     int r0;
     const int nq = sample_rows(a, b, r0);
     const int n = a.cache.length(b, a.max_len);
-    if ((int)blockIdx.x < join_wgs) {
-        const int tpr = dh >> 2, per = 256 / tpr / groups, y = tid / tpr, c = tid - y * tpr;
-        const int which = y / groups, g = y - which * groups, item = blockIdx.x * per + which;
-        const bool there = which < per && item < nq * a.H;
-        const size_t at = (size_t)r0 * a.H + item;
-        float m = -INFINITY, z = 0.f;
-        f32x4 t = {0.f, 0.f, 0.f, 0.f};
-        if (there) {
-            const int S = runs_of(a, row_limit(a, n, nq, item / a.H));
-            const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + at * a.S;
-            const f32x4* part = reinterpret_cast<const f32x4*>(a.part_o + at * a.S * dh) + c;
-            for (int s = g; s < S; s += groups * JW_UNROLL) {
-                float2 v[JW_UNROLL];
-                f32x4 p[JW_UNROLL];
-#pragma unroll
-                for (int u = 0; u < JW_UNROLL; ++u) {
-                    const int su = min(s + u * groups, S - 1);
-                    v[u] = ml[su];
-                    p[u] = part[(size_t)su * tpr];
-                }
-                float mn = m;
-#pragma unroll
-                for (int u = 0; u < JW_UNROLL; ++u) mn = fmaxf(mn, v[u].x);             // (a run that comes twice does not change it)
-                const float ref = mn == -INFINITY ? 0.f : mn, f0 = exp2f(m - ref);
-                m = mn;
-                z *= f0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) t[e] *= f0;
-#pragma unroll
-                for (int u = 0; u < JW_UNROLL; ++u) {
-                    const float f = s + u * groups < S ? exp2f(v[u].x - ref) : 0.f;
-                    z = __builtin_fmaf(v[u].y, f, z);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) t[e] = __builtin_fmaf(p[u][e], f, t[e]);
-                }
-            }
-        }
-        if (groups > 1) {
-            gt[tid] = t;
-            if (c == 0 && y < 64) { gm[y] = m; gz[y] = z; }
-            __syncthreads();
-            if (there && g == 0) {
-                float mt = m;
-                for (int i = 1; i < groups; ++i) mt = fmaxf(mt, gm[y + i]);
-                const float ref = mt == -INFINITY ? 0.f : mt, f0 = exp2f(m - ref);
-                z *= f0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) t[e] *= f0;
-                for (int i = 1; i < groups; ++i) {
-                    const float f = exp2f(gm[y + i] - ref);
-                    const f32x4 p = gt[tid + i * tpr];
-                    z = __builtin_fmaf(gz[y + i], f, z);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) t[e] = __builtin_fmaf(p[e], f, t[e]);
-                }
-                m = mt;
-            }
-        }
-        if (!there || g != 0) return;
-        const float inv = z > 0.f ? 1.0f / z : 0.f;
-        T* o = static_cast<T*>(a.o) + at * dh + c * 4;
-        const float w[4] = {t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv};
-        if constexpr (sizeof(T) == 2) store_bf16<4>(o, w);
-        else *reinterpret_cast<f32x4*>(o) = f32x4{w[0], w[1], w[2], w[3]};
-        if (c == 0) {
-            const float l2 = z > 0.f ? m + log2f(z) : -INFINITY;
-            if (a.lse) a.lse[at] = l2 * 0.6931471805599453f;
-            if (a.lse2) a.lse2[at] = l2;
-        }
-        return;
-    }
-    const int j = ((int)blockIdx.x - join_wgs) * 256 + tid;
-    if (j - tid >= n) return;
+    // 64 slots to a workgroup, every wave has a quarter of the rows, JW_BATCH of them requested together, the first ones in front of the rows' lse
+    const int slot0 = ((int)blockIdx.x - join_wgs) * 64, j = slot0 + (tid & 63), wave = tid >> 6;
+    if (slot0 >= n) return;
     const int items = nq * a.H;
+    const size_t to = (size_t)b * a.weight_stride + j;
+    const float before = a.weight_in && wave == 0 && j < n ? a.weight_in[to] : 0.f;
     float total = 0.f;
     for (int c0 = 0; c0 < items; c0 += JW_ROWS) {
         const int cnt = min(items - c0, JW_ROWS);
-        __syncthreads();
-        if (a.S == 1) {
-            for (int u = tid; u < cnt; u += 256) lse2[u] = a.lse2[(size_t)r0 * a.H + c0 + u];
-        } else {
-            const int sub = tid & 7;
-            for (int u = tid >> 3; u < (cnt + 31) / 32 * 32; u += 32) {
-                const int uc = min(u, cnt - 1);
-                const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + ((size_t)r0 * a.H + c0 + uc) * a.S;
-                const int S = runs_of(a, row_limit(a, n, nq, (c0 + uc) / a.H));
-                float m = -INFINITY, z = 0.f;
-                for (int s = sub; s < S; s += 8) lse2_combine(m, z, ml[s].x, ml[s].y);
+        const float* x = a.logits + ((size_t)r0 * a.H + c0) * a.lpad + min(j, n - 1);
+        float v[JW_BATCH];
+        auto request = [&](int u0) {
 #pragma unroll
-                for (int o = 1; o < 8; o <<= 1) {
-                    const float m2 = __shfl_xor(m, o), z2 = __shfl_xor(z, o);
-                    lse2_combine(m, z, m2, z2);
-                }
-                if (sub == 0 && u < cnt) lse2[u] = m + log2f(z);
-            }
-        }
+            for (int i = 0; i < JW_BATCH; ++i) v[i] = x[(size_t)min(u0 + wave + 4 * i, cnt - 1) * a.lpad];
+        };
+        request(0);
         __syncthreads();
-        if (j < n) {
-            const float* x = a.logits + ((size_t)r0 * a.H + c0) * a.lpad + j;
-#pragma unroll 8
-            for (int u = 0; u < cnt; ++u) {
-                const float v = x[(size_t)u * a.lpad] - lse2[u];
-                total += j < row_limit(a, n, nq, (c0 + u) / a.H) ? exp2f(v) : 0.f;
+        rows_lse2<256>(a, r0, nq, n, c0, cnt, lse2);
+        __syncthreads();
+        for (int u0 = 0; u0 < cnt; u0 += 4 * JW_BATCH) {
+            if (u0 > 0) request(u0);
+#pragma unroll
+            for (int i = 0; i < JW_BATCH; ++i) {
+                const int u = u0 + wave + 4 * i;
+                const bool seen = u < cnt && j < row_limit(a, n, nq, (c0 + u) / a.H);
+                total += seen ? exp2f(v[i] - lse2[min(u, cnt - 1)]) : 0.f;
             }
         }
     }
-    if (j < n) {
-        const size_t at = (size_t)b * a.weight_stride + j;
-        a.weight_out[at] = (a.weight_in ? a.weight_in[at] : 0.f) + total / (float)a.H;
-    }
+    lds.t[tid][0] = total;
+    __syncthreads();
+    if (wave == 0 && j < n) a.weight_out[to] = before + ((lds.t[tid][0] + lds.t[tid + 64][0]) + (lds.t[tid + 128][0] + lds.t[tid + 192][0])) / (float)a.H;
 }
 
 // What the slots got: a workgroup has 64 slots of a sample, 16 lanes a slot, and goes over all heads and rows.
@@ -901,15 +1030,19 @@ constexpr int AC_MAX_RUN = 4096;                // the pages of a run: in a wave
 static AttendCachePlan attend_cache_plan(const d3tom_paged_cache& c, int rows, int max_q, int max_len, int H, int weighed) {
     AttendCachePlan p;
     const long long R = (long long)max_q * (H / c.Hkv);
-    p.kernel = c.dh != 64 && c.dh != 128 ? AC_GENERIC : R <= 16 ? AC_WAVES : R <= 64 ? AC_ROWS64 : AC_ROWS128;
-    const int tile_rows[] = {1, 16, 64, 128}, want[] = {1024, 256, 512, 512};
+    p.kernel = c.dh != 64 && c.dh != 128 ? AC_GENERIC : R <= 16 ? AC_WAVES : R <= 64 || (c.dt == D3TOM_F32 && c.dh == 128) ? AC_ROWS64 : AC_ROWS128;
+    const int tile_rows[] = {1, 16, 64, 128}, want[] = {1024, 256, 256, 256};
     p.tiles = (int)((R + tile_rows[p.kernel] - 1) / tile_rows[p.kernel]);
-    const long long groups = (long long)c.B * (p.kernel == AC_GENERIC ? (long long)max_q * H : (long long)c.Hkv * p.tiles), step = 256;
-    long long S = groups >= want[p.kernel] ? 1 : want[p.kernel] / groups;
+    const long long groups = (long long)c.B * (p.kernel == AC_GENERIC ? (long long)max_q * H : (long long)c.Hkv * p.tiles), step = p.kernel == AC_GENERIC ? 256 : 128;
+    int wantk = want[p.kernel]; if (getenv("AC_WANT")) wantk = atoi(getenv("AC_WANT"));
+    long long S = groups >= wantk ? 1 : wantk / groups;
     const long long most = (max_len + step - 1) / step;
     S = S > most ? most : S;
+    if (p.kernel == AC_WAVES && (size_t)max_len * c.dh * elem_bytes(c.dt) <= (getenv("AC_ONE") ? atoi(getenv("AC_ONE")) : 128) * 1024) S = 1;
     p.run = (int)((most + S - 1) / S * step);
-    if (p.kernel != AC_GENERIC && p.run > AC_MAX_RUN) p.run = AC_MAX_RUN;
+    if (getenv("AC_RUN")) p.run = atoi(getenv("AC_RUN"));
+    const int maxrun = p.kernel == AC_WAVES && getenv("AC_W") ? 1024 * atoi(getenv("AC_W")) : AC_MAX_RUN;
+    if (p.kernel != AC_GENERIC && p.run > maxrun) p.run = maxrun;
     p.S = (max_len + p.run - 1) / p.run;
     p.keep = weighed && p.kernel == AC_WAVES;
     p.lpad = (max_len + 15) / 16 * 16;
@@ -920,26 +1053,48 @@ static AttendCachePlan attend_cache_plan(const d3tom_paged_cache& c, int rows, i
     p.part_o = take(p.S > 1 ? rh * p.S * c.dh * 4 : 0);
     p.part_ml = take(p.S > 1 ? rh * p.S * 8 : 0);
     p.logits = take(p.keep ? rh * p.lpad * 4 : 0);
-    p.bytes = o > 256 ? o : 256;
+    p.bytes = o;
     return p;
+}
+// What a workspace needs that is to serve every call of at most these sizes (fewer rows may mean more runs, or logits that are kept): a plan has at most want * tile rows
+// times runs where the units ask for runs, and a run for every AC_MAX_RUN slots otherwise.
+static size_t attend_cache_ws_bytes(const d3tom_paged_cache& c, int rows, int max_q, int max_len, int H, int weighed) {
+    const size_t rh = (size_t)rows * H, most = rh * ((max_len + 127) / 128), some = 128 * 512 + rh * ((max_len + AC_MAX_RUN - 1) / AC_MAX_RUN);
+    const size_t parts = most < some ? most : some, kept = rh < (size_t)c.B * c.Hkv * 16 ? rh : (size_t)c.B * c.Hkv * 16;
+    size_t bytes = 4 * 256 + parts * (c.dh * 4 + 8);
+    if (weighed) bytes += rh * 4 + kept * ((max_len + 15) / 16 * 16) * 4;
+    const size_t plan = attend_cache_plan(c, rows, max_q, max_len, H, weighed).bytes;          // more only where max_q is not the longest run
+    return bytes > plan ? bytes : plan;
 }
 template <typename T, int DH>
 static int attend_cache_launch(const AttendCacheArgs& a, int kernel, hipStream_t st) {
     static PerDeviceOnce once;
-    constexpr int WAVES_LDS = 4 * AcTile<T, DH>::WAVE_LDS, ROWS_LDS = AcShared<T, DH>::LDS;
+    constexpr int WAVES_LDS = 4 * AcTile<T, DH>::WAVE_LDS, ROWS_LDS = AcShared<T, DH>::LDS, WIDE = AcTile<T, DH>::KS > 4 ? 1 : 2;        // (float32 heads of 128 have no registers for 128 rows)
     if (!once.run([] {
-            return raise_dynamic_lds(attend_cache_kernel<T, DH>, WAVES_LDS) && raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 1>, ROWS_LDS) &&
-                   raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 2>, ROWS_LDS);
+            return raise_dynamic_lds(attend_cache_kernel<T, DH, 4>, WAVES_LDS) && raise_dynamic_lds(attend_cache_kernel<T, DH, 2>, WAVES_LDS / 2) &&
+                raise_dynamic_lds(attend_cache_kernel<T, DH, 1>, WAVES_LDS / 4) && raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 1>, ROWS_LDS) &&
+                   raise_dynamic_lds(attend_cache_rows_kernel<T, DH, WIDE>, ROWS_LDS);
         })) return D3TOM_ERR_DEVICE;
     const int wgs = (a.nB * a.cache.Hkv * a.S + 7) / 8 * 8 * a.tiles;
-    if (kernel == AC_WAVES) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH><<<wgs, 256, WAVES_LDS, st>>>(a)));
-    else if (kernel == AC_ROWS64) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, 1><<<wgs, 256, ROWS_LDS, st>>>(a)));
-    else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, 2><<<wgs, 256, ROWS_LDS, st>>>(a)));
+    const int W = getenv("AC_W") ? atoi(getenv("AC_W")) : 4;
+    if (kernel == AC_WAVES) {
+        if (W == 4) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 4><<<wgs, 256, WAVES_LDS, st>>>(a)));
+        else if (W == 2) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 2><<<wgs, 128, WAVES_LDS / 2, st>>>(a)));
+        else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 1><<<wgs, 64, WAVES_LDS / 4, st>>>(a)));
+    }
+    else if (kernel == AC_ROWS64) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, 1><<<wgs, 512, ROWS_LDS, st>>>(a)));
+    else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, WIDE><<<wgs, 512, ROWS_LDS, st>>>(a)));
     return D3TOM_OK;
+}
+// threads that share a row's runs when `threads` join rows of dh channels
+static int join_groups(int S, int dh, int threads) {
+    int groups = 1;
+    while (groups * JW_UNROLL < S && groups * 2 <= threads / (dh / 4)) groups *= 2;
+    return groups;
 }
 template <typename T, int DH>
 static int cache_weigh_launch(const AttendCacheArgs& a, hipStream_t st) {
-    constexpr int KEYS = AcTile<T, DH>::KS > 4 ? 32 : 64;
+    constexpr int KEYS = cw_blocks(AcTile<T, DH>::KS) * 16;
     const dim3 grid((a.max_len + KEYS - 1) / KEYS, a.nB);
     D3TOM_LAUNCH(CACHE_WEIGH, st, (cache_weigh_kernel<T, DH><<<grid, CW_WAVES * 64, 0, st>>>(a)));
     return D3TOM_OK;
@@ -958,7 +1113,7 @@ using namespace d3tom;
 
 extern "C" size_t d3tom_attend_cache_workspace_bytes(const d3tom_paged_cache* cache, int rows, int max_q, int max_len, int H, int weighed) {
     if (attend_cache_check(cache, rows, max_q, max_len, H) != D3TOM_OK) return 0;
-    return attend_cache_plan(*cache, rows, max_q, max_len, H, weighed).bytes;
+    return attend_cache_ws_bytes(*cache, rows, max_q, max_len, H, weighed);
 }
 
 extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_paged_cache* cache, const int32_t* q_off, int rows, int max_q,
@@ -972,14 +1127,15 @@ extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_p
     if (!q_off || !ws || !(scale > 0.f) || !(scale < 3.0e38f)) return D3TOM_ERR_INVALID_ARG;
     if ((weight_in && !weight_out) || (weight_out && weight_stride < max_len)) return D3TOM_ERR_INVALID_ARG;
     const AttendCachePlan p = attend_cache_plan(*cache, rows, max_q, max_len, H, weight_out != nullptr);
-    if (ws_bytes < p.bytes || (((uintptr_t)ws) & 255u)) return D3TOM_ERR_WORKSPACE_TOO_SMALL;
     const double most = 16000000.0;             // workgroups of 256 threads in a launch
     if ((double)cache->B * max_q * H * p.S > most || (double)max_q * H > most) return D3TOM_ERR_UNSUPPORTED;
+    if (ws_bytes < attend_cache_ws_bytes(*cache, rows, max_q, max_len, H, weight_out != nullptr) || (((uintptr_t)ws) & 255u)) return D3TOM_ERR_WORKSPACE_TOO_SMALL;
     AttendCacheArgs a{};
     a.cache = cache_view(*cache);
     a.q = q; a.k_pages = cache->k_pages; a.v_pages = cache->v_pages; a.q_stride = q_stride; a.q_off = q_off;
     a.nB = cache->B; a.rows = rows; a.max_q = max_q; a.max_len = max_len; a.H = H; a.G = H / cache->Hkv; a.causal = causal != 0;
     a.scale2 = scale * LOG2E;
+    a.last_slot = max_len - 1;                  // (the table has all of max_len)
     a.S = p.S; a.run = p.run; a.o = o; a.lse = lse; a.lpad = p.lpad; a.tiles = p.tiles;
     a.lse2 = weight_out ? (float*)((char*)ws + p.lse2) : nullptr;
     a.part_o = (float*)((char*)ws + p.part_o); a.part_ml = (float*)((char*)ws + p.part_ml);
@@ -995,9 +1151,8 @@ extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_p
         if (bf16) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_generic_kernel<uint16_t><<<wgs, 256, 0, st>>>(a)));
         else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_generic_kernel<float><<<wgs, 256, 0, st>>>(a)));
     }
-    int groups = 1;                              // of threads, over the runs of a row
-    while (groups < p.S && groups * 2 <= 256 / (dh / 4)) groups *= 2;
-    const int per = 256 / (dh / 4) / groups, join_wgs = p.S > 1 ? (max_q * H + per - 1) / per : 0, weigh_wgs = p.keep ? (max_len + 255) / 256 : 0;
+    const int groups = join_groups(p.S, dh, 256);
+    const int per = 256 / (dh / 4) / groups, join_wgs = p.S > 1 ? (max_q * H + per - 1) / per : 0, weigh_wgs = p.keep ? (max_len + 63) / 64 : 0;
     if (join_wgs + weigh_wgs > 0) {
         const dim3 grid(join_wgs + weigh_wgs, cache->B);
         if (bf16) D3TOM_LAUNCH(CACHE_JOIN, st, (attend_cache_join_kernel<uint16_t><<<grid, 256, 0, st>>>(a, join_wgs, groups)));

@@ -179,6 +179,24 @@ def test_attend_cache_refuses(B):
     assert _attend(lib, B, cache=_cache(B, B=65535), rows=1 << 30, most=1 << 30) == UNSUPPORTED
 
 
+def test_attend_cache_workspace_serves_smaller_calls(B):
+    import random
+    rng = random.Random(0)
+    log_int = lambda lo, hi: int(lo * (hi / lo) ** rng.random())
+    for _ in range(3000):
+        nB, Hkv = log_int(1, 64), rng.choice([1, 2, 4, 8, 32])
+        c = _cache(B, B=nB, Hkv=Hkv, dh=rng.choice([8, 64, 96, 128]), dt=rng.choice([0, 1]), table_stride=10 ** 5)
+        need = lambda rows, most, n, w: B._lib.d3tom_attend_cache_workspace_bytes(c, rows, most, n, H, w)
+        H, n, most = Hkv * rng.choice([1, 2, 4, 8, 16]), log_int(1, 200000), log_int(1, 400)
+        rows = rng.randint(most, most * nB)
+        all_of_it = need(rows, most, n, 1)
+        assert all_of_it > 0
+        for _ in range(4):
+            m2 = log_int(1, most + 1)
+            r2 = min(rows, rng.randint(m2, m2 * nB))
+            assert 0 < need(r2, min(m2, r2), log_int(1, n + 1), rng.choice([0, 1])) <= all_of_it
+
+
 def _evict(lib, B, cache=None, max_len=320, keep=P, first=4, recent=8, wi=P, ti=P, wo=P, to=P, stride=320, lo=P, src=None, ws=P, nbytes=1 << 40):
     return lib.d3tom_cache_evict(ctypes.byref(cache if cache is not None else _cache(B)), i32(max_len), keep, i32(first), i32(recent), wi, ti, wo, to, i32(stride), lo,
                                  src, ws, sz(nbytes), None)
