@@ -524,7 +524,7 @@ int d3tom_cache_append(const d3tom_paged_cache* cache /* host */, const void* k,
  * (row i of n: slot kv_len[b] - n + i).  A row that sees no slot gets zeros and lse -infinity.  What lies behind a sample's last
  * slot is never used, NaN included.
  *
- *   q          [rows, H, dh] dt, q_stride elements between rows (a multiple of 16 bytes); H a multiple of Hkv
+ *   q          [rows, H, dh] dt, q_stride elements between rows (a multiple of 16 bytes, at most 16 MB); H a multiple of Hkv
  *   q_off      int32[B + 1]  first row of each sample; rows = q_off[B] (host-known), max_q the longest run, max_len the longest cache
  *   o          [rows, H, dh] dt contiguous, out           lse  float[rows, H] out or NULL: log sum exp of the row's logits
  *   weight_out float[B, weight_stride] out or NULL: for every live slot weight_in plus the probabilities that the sample's rows give
@@ -532,7 +532,8 @@ int d3tom_cache_append(const d3tom_paged_cache* cache /* host */, const void* k,
  *   weight_in  float[B, weight_stride] or NULL (zeros); may be weight_out
  * bf16: the probabilities enter the product with v as bf16, relative to the running maximum of their row, all sums are float32.
  * Long caches are cut into runs of slots whose results are joined; how goes by the host-known sizes only, so that a call has
- * the same bits whatever the cache's unused slots hold.  No size is a limit but: rows * H and B * H at most 2^31 - 1 workgroups.
+ * the same bits whatever the cache's unused slots hold.  Calls of more than 16 million workgroups
+ * (samples * max_q * H times the runs of a cache) return D3TOM_ERR_UNSUPPORTED.
  * Workspace: d3tom_attend_cache_workspace_bytes (weighed: whether weight_out is given; 0 for arguments that the call refuses), which is
  * enough for every call on the cache with at most these rows, max_len and H, weighed or not, whatever max_q.
  * ---------------------------------------------------------------------------------------- */

@@ -184,9 +184,6 @@ __device__ __forceinline__ f32x4 ac_mma(const uint4& a, const uint4& b, f32x4 c)
         return c;
     }
 }
-// Makes a load's result be there at this point.  The compiler does not count the direct loads: a register whose load it has not seen the end of in front of the loop would be
-// waited for in every turn, by a wait for everything that is on its way.
-__device__ __forceinline__ void arrived(uint4& v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
 __device__ __forceinline__ float quad_max(float v) { return quad_combine(v, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float quad_sum(float v) { return quad_combine(v, [](float a, float b) { return a + b; }); }
 #endif
@@ -274,12 +271,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
     const int mine = (ntile - wave + WAVES - 1) / WAVES;                                       // tiles wave, wave + WAVES, ...
     const uint32_t ids = a.cache.readable(my_page);
 
-    uint4 qf[KS];
-    {
-        const char* q = static_cast<const char*>(a.q) + (row * a.q_stride + (size_t)xh * DH) * sizeof(T);
-#pragma unroll
-        for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const uint4*>(q + (kk * 4 + g) * 16);
-    }
     const uint32_t row_bytes = (uint32_t)a.cache.row_elems() * sizeof(T);
     const int ld_pos = lane % NCHK, ld_row = lane / NCHK;
     int k_off[LDB], v_off[LDB];
@@ -306,8 +297,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
     };
     auto issue_k = [&](int t) { issue(kbase, k_off, t, ring0 + (t & 1) * C::STAGE); };
     auto issue_v = [&](int t) { issue(vbase, v_off, t, ring0 + (t & 1) * C::STAGE + C::TILE); };
+    // The queries in front of them, on the same way: sixteen rows whose place in LDS all waves share, behind the rings.  (Loaded as fragments into registers, 64
+    // bytes of a row at a time, they are slower than the keys, and these waited for them: 1 us.)
+    const uint32_t q_lds = (uint32_t)(size_t)(lds_ptr_t)ring + WAVES * C::WAVE_LDS;
+    constexpr int QLD = 16 / RPI;
+    const __amdgpu_buffer_rsrc_t rq = make_uniform_rsrc(static_cast<const char*>(a.q) + ((size_t)(r0 + R0 / a.G) * a.q_stride + (size_t)kvh * a.G * DH) * sizeof(T), ~0u);
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk) arrived(qf[kk]);
+    for (int i = 0; i < (QLD + WAVES - 1) / WAVES; ++i) {
+        const int li = i * WAVES + wave;
+        if (QLD % WAVES == 0 || li < QLD) {
+            const int x2 = li * RPI + ld_row, X = min(R0 + x2, R - 1), Xi = X / a.G;
+            direct_load_16(rq, (uint32_t)((Xi - R0 / a.G) * (int)a.q_stride + (X - Xi * a.G) * DH) * sizeof(T) + ((ld_pos ^ C::k_turn(x2)) << 4), q_lds + li * 1024);
+        }
+    }
     issue_k(0); issue_v(0); issue_k(1); issue_v(1);
 
     int k_addr[KS], v_addr[DB];
@@ -326,6 +328,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
 #pragma unroll
     for (int t = 0; t < DB; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
+    wait_loads_and_barrier<4 * C::LD>();                       // the queries are there
+    uint4 qf[KS];
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const uint4*>(ring + WAVES * C::WAVE_LDS + k_addr[kk]);
     float* kept = a.logits ? a.logits + (row * a.H + xh) * a.lpad : nullptr;
     const bool real = R0 + r < R;
 
@@ -483,13 +489,6 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
     const int limit0 = min(row_limit(a, n, nq, min(W0, R - 1) / a.G), j1);
     const int ntile = j1 > j0 ? (j1 - j0 + KEYS - 1) / KEYS : 0;
     if (tid < W::PAGES) pages[tid] = a.cache.readable(my_page);
-    uint4 qf[QB][KS];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const char* q = static_cast<const char*>(a.q) + (row[qb] * a.q_stride + (size_t)xh[qb] * DH) * sizeof(T);
-#pragma unroll
-        for (int kk = 0; kk < KS; ++kk) qf[qb][kk] = *reinterpret_cast<const uint4*>(q + (kk * 4 + g) * 16);
-    }
     const uint32_t row_bytes = (uint32_t)a.cache.row_elems() * sizeof(T);
     const int ld_pos = lane % NCHK, ld_row = lane / NCHK;
     const uint32_t ring0 = (uint32_t)(size_t)(lds_ptr_t)ring;
@@ -517,13 +516,27 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
         }
     };
     auto pages_of = [&](int t) { return pages[min(t * KB + (lane & (KB - 1)), W::PAGES - 1)]; };
+    // the queries lie where tiles 2 and 3 will
+    constexpr int QLD = ROWS / RPI / 8;
+    {
+        const __amdgpu_buffer_rsrc_t rq = make_uniform_rsrc(static_cast<const char*>(a.q) + ((size_t)(r0 + R0 / a.G) * a.q_stride + (size_t)kvh * a.G * DH) * sizeof(T), ~0u);
+#pragma unroll
+        for (int i = 0; i < QLD; ++i) {
+            const int x = (wave * QLD + i) * RPI + ld_row, X = min(R0 + x, R - 1), Xi = X / a.G;
+            direct_load_16(rq, (uint32_t)((Xi - R0 / a.G) * (int)a.q_stride + (X - Xi * a.G) * DH) * sizeof(T) + ((ld_pos ^ C::k_turn(x & 15)) << 4),
+                           ring0 + 2 * W::STAGE + (wave * QLD + i) * 1024);
+        }
+    }
     __syncthreads();
+    issue(0, pages_of(0));
+    issue(1, pages_of(1));
+    wait_loads_and_barrier<2 * 2 * LD>();              // the queries are there
+    uint4 qf[QB][KS];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-        for (int kk = 0; kk < KS; ++kk) arrived(qf[qb][kk]);
-    issue(0, pages_of(0));
-    issue(1, pages_of(1));
+        for (int kk = 0; kk < KS; ++kk)
+            qf[qb][kk] = *reinterpret_cast<const uint4*>(ring + 2 * W::STAGE + ((rg * QB + qb) * 16 + r) * ROWB + (((kk * 4 + g) ^ C::k_turn(r)) << 4));
 
     int k_addr[KS], v_addr[DB];
     const int half = kg * KW * 16 * ROWB;              // this wave's keys of a tile
@@ -813,16 +826,24 @@ __device__ __forceinline__ void rows_lse2(const AttendCacheArgs& a, int r0, int 
 
 // What the slots got where the logits are not kept: they are formed again, K Q^T once more (the keys' rows a third time through memory is less than
 // 4 bytes a logit there and back).  A workgroup has a tile of a sample's slots and goes over all heads and rows, wave w over key heads w, w + 8, ...
-// (or parts of a head's rows where there are fewer); the keys of a head lie in its registers, the queries come from the caches, one block of 16 rows ahead.  Bound by vector
-// instructions: an fma, an exp2 and an addition a logit.  (The rows' lse come from the joining launch in front: formed by every workgroup for itself in one launch with
-// the joining, four samples of 128 rows to a key head took 27 us instead of 21.)
+// (or parts of a head's rows where there are fewer), each wave on its own.  The keys of a head come through LDS into its registers, then the queries, 16 rows at a time with
+// their lse, through a ring in the same place.  (Loaded as fragments, 64 bytes of a row at a time, the keys took 6700 clocks and every block of queries 2000.)
+// In the end bound by vector instructions: an fma, an exp2 and an addition a logit.  (The rows' lse come from the joining launch in front: formed by every
+// workgroup for itself in one launch with the joining, four samples of 128 rows to a key head took 27 us instead of 21.)
 constexpr int CW_WAVES = 8;
-constexpr int cw_blocks(int ks) { return ks > 4 ? 2 : 4; }            // of 16 keys, in registers
+template <typename T, int DH> struct CwTile {
+    using C = AcTile<T, DH>;
+    static constexpr int KB = C::KS > 4 ? 2 : 4, KEYS = KB * 16;                            // of a wave's registers
+    static constexpr int QROWS = 16 * C::ROWB, SLOT = QROWS + 256, SLOTS = C::KS > 4 ? 2 : 4;       // queries of a block, and 64 words of lse
+    static constexpr int WAVE_LDS = SLOTS * SLOT > KEYS * C::ROWB ? SLOTS * SLOT : KEYS * C::ROWB, LDS = CW_WAVES * WAVE_LDS;
+};
 template <typename T, int DH>
-__global__ __launch_bounds__(CW_WAVES * 64) void cache_weigh_kernel(AttendCacheArgs a) {
+__global__ __launch_bounds__(CW_WAVES * 64, 2) void cache_weigh_kernel(AttendCacheArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = AcTile<T, DH>;
-    constexpr int KS = C::KS, KB = cw_blocks(KS), KEYS = KB * 16;
+    using W = CwTile<T, DH>;
+    constexpr int KS = C::KS, KB = W::KB, KEYS = W::KEYS, ROWB = C::ROWB, NCHK = C::NCHK, RPI = C::RPI, LDB = C::LDB, SLOTS = W::SLOTS;
+    extern __shared__ __attribute__((aligned(16))) char ring[];
     __shared__ float sums[CW_WAVES][KEYS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     const int b = blockIdx.y, key0 = blockIdx.x * KEYS;
@@ -836,52 +857,88 @@ __global__ __launch_bounds__(CW_WAVES * 64) void cache_weigh_kernel(AttendCacheA
     const int jt = key0 + tid;
     const size_t to = (size_t)b * a.weight_stride + jt;
     const float before = tid < KEYS && jt < n && a.weight_in ? a.weight_in[to] : 0.f;
-    const size_t row_bytes = a.cache.row_elems() * sizeof(T);
-    const char* kp[KB];
+    const uint32_t row_bytes = (uint32_t)a.cache.row_elems() * sizeof(T);
+    const int ld_pos = lane % NCHK, ld_row = lane / NCHK;
+    const uint32_t mine = (uint32_t)(size_t)(lds_ptr_t)ring + wave * W::WAVE_LDS;
+    const char* at = ring + wave * W::WAVE_LDS;
+    int k_off[LDB], q_addr[KS];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-        const int at = min(key0 + kb * 16, (n - 1) & ~15), j = min(at + r, n - 1);         // blocks behind the last one: that one again
-        const int p = at == key0 + kb * 16 ? page[kb] : a.cache.page_of(b, at);
-        kp[kb] = static_cast<const char*>(a.k_pages) + a.cache.row(a.cache.readable(p), j) * row_bytes + g * 16;
+    for (int i = 0; i < LDB; ++i) {
+        const int x = i * RPI + ld_row;
+        k_off[i] = x * row_bytes + ((ld_pos ^ C::k_turn(x)) << 4);
     }
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) q_addr[kk] = r * ROWB + (((kk * 4 + g) ^ C::k_turn(r)) << 4);
     f32x4 acc[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) acc[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int parts = a.cache.Hkv >= CW_WAVES ? 1 : (CW_WAVES + a.cache.Hkv - 1) / a.cache.Hkv;
-    const int step_i = parts * 16 / a.G, step_x = parts * 16 - step_i * a.G;               // rows and heads from one block to the next
-    uint4 kf[KB][KS];
-    auto keys = [&](int kvh) {
+    const int parts = a.cache.Hkv >= CW_WAVES ? 1 : (CW_WAVES + a.cache.Hkv - 1) / a.cache.Hkv, step = parts * 16;
+    const int step_i = step / a.G, step_x = step - step_i * a.G;                            // rows and heads from one block to the next
+    for (int it = wave; it < a.cache.Hkv * parts; it += CW_WAVES) {
+        const int kvh = it / parts, first = (it - kvh * parts) * 16;
+        if (first >= R) continue;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const int slot = key0 + kb * 16, there = min(max(n - slot, 0), 16);
+            const uint32_t p = a.cache.readable(__builtin_amdgcn_readfirstlane(page[kb]));
+            const __amdgpu_buffer_rsrc_t rk = make_uniform_rsrc(static_cast<const char*>(a.k_pages) + a.cache.row(p, slot) * row_bytes + (size_t)kvh * ROWB,
+                                                                there ? (uint32_t)(there - 1) * row_bytes + ROWB : 0u);
+#pragma unroll
+            for (int i = 0; i < LDB; ++i) direct_load_16(rk, k_off[i], mine + (kb * LDB + i) * 1024);
+        }
+        wait_loads<0>();
+        uint4 kf[KB][KS];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int kk = 0; kk < KS; ++kk) kf[kb][kk] = *reinterpret_cast<const uint4*>(kp[kb] + (size_t)kvh * C::ROWB + kk * 64);
-    };
-    for (int it = wave; it < a.cache.Hkv * parts; it += CW_WAVES) {
-        const int kvh = it / parts, part = it - kvh * parts;
-        if (part * 16 >= R) continue;
-        keys(kvh);
-        // this lane's row and head of the block that is requested next
-        int xi = (part * 16 + r) / a.G, xr = part * 16 + r - xi * a.G;
-        uint4 qf[KS];
-        float lse2;
-        int limit;
-        auto request = [&]() {
-            const int i = min(xi, nq - 1);
-            lse2 = a.lse2[(size_t)(r0 + i) * a.H + kvh * a.G + xr];
-            limit = xi < nq ? row_limit(a, n, nq, xi) : 0;
-            const char* q = static_cast<const char*>(a.q) + ((size_t)(r0 + i) * a.q_stride + (size_t)(kvh * a.G + xr) * DH) * sizeof(T) + g * 16;
+            for (int kk = 0; kk < KS; ++kk) kf[kb][kk] = *reinterpret_cast<const uint4*>(at + kb * 16 * ROWB + q_addr[kk]);
+        wait_lds();
+        // The block that is requested next: its first row, and (row, head) of this lane's rows in the loads and of its column, all moving on together.
+        int x0 = first, i0 = first / a.G, li[LDB], lx[LDB], ci, cx;
 #pragma unroll
-            for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const uint4*>(q + kk * 64);
-            xi += step_i;
-            xr += step_x;
-            if (xr >= a.G) { xr -= a.G; ++xi; }
+        for (int i = 0; i < LDB; ++i) {
+            const int x = first + i * RPI + ld_row;
+            li[i] = x / a.G;
+            lx[i] = x - li[i] * a.G;
+        }
+        ci = (first + r) / a.G;
+        cx = first + r - ci * a.G;
+        int rest = first - i0 * a.G;
+        int seen_i = ci;                                // row of this lane's column in the block that is used next
+        auto request = [&](int s) {
+            const size_t row = (size_t)(r0 + i0);
+            const uint32_t all = x0 < R ? ~0u : 0u;     // (a block that there is not: no memory is touched, the loads are counted)
+            const __amdgpu_buffer_rsrc_t rq = make_uniform_rsrc(static_cast<const char*>(a.q) + (row * a.q_stride + (size_t)kvh * a.G * DH) * sizeof(T), all);
+            const __amdgpu_buffer_rsrc_t rl = make_uniform_rsrc(a.lse2 + row * a.H + (size_t)kvh * a.G, all);
+#pragma unroll
+            for (int i = 0; i < LDB; ++i) {
+                const uint32_t off = (uint32_t)((min(li[i], nq - 1) - i0) * (int)a.q_stride + lx[i] * DH) * sizeof(T);
+                const int x = i * RPI + ld_row;
+                direct_load_16(rq, off + ((ld_pos ^ C::k_turn(x)) << 4), mine + s * W::SLOT + i * 1024);
+                li[i] += step_i; lx[i] += step_x;
+                if (lx[i] >= a.G) { lx[i] -= a.G; ++li[i]; }
+            }
+            direct_load_4(rl, (uint32_t)((min(ci, nq - 1) - i0) * a.H + cx) * 4u, mine + s * W::SLOT + W::QROWS);
+            ci += step_i; cx += step_x;
+            if (cx >= a.G) { cx -= a.G; ++ci; }
+            x0 += step; i0 += step_i; rest += step_x;
+            if (rest >= a.G) { rest -= a.G; ++i0; }
         };
-        request();
-        // (two different texts, for the compiler: the requests in front of the loop and in it would otherwise become one, at the loop's top, behind the products)
-        asm volatile("; first rows" ::: "memory");
-        for (int x0 = part * 16; x0 < R; x0 += parts * 16) {
-            const float ref = lse2;
-            const int seen = limit - key0 - 4 * g;
+        int seen_x = cx;
+#pragma unroll
+        for (int s = 0; s < SLOTS - 1; ++s) request(s);
+        int s = 0;
+        for (int x = first; x < R; x += step) {
+            wait_loads<(SLOTS - 2) * (LDB + 1)>();      // this block is there
+            request(s == 0 ? SLOTS - 1 : s - 1);
+            const char* w = at + s * W::SLOT;
+            uint4 qf[KS];
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const uint4*>(w + q_addr[kk]);
+            const float ref = *reinterpret_cast<const float*>(w + W::QROWS + lane * 4);
+            const int limit = seen_i < nq ? row_limit(a, n, nq, seen_i) : 0, seen = limit - key0 - 4 * g;
+            seen_i += step_i; seen_x += step_x;
+            if (seen_x >= a.G) { seen_x -= a.G; ++seen_i; }
             const bool masked = __builtin_amdgcn_ballot_w64(limit < key0 + KEYS) != 0;
             f32x4 st[KB];
 #pragma unroll
@@ -890,8 +947,6 @@ __global__ __launch_bounds__(CW_WAVES * 64) void cache_weigh_kernel(AttendCacheA
             for (int kk = 0; kk < KS; ++kk)
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) st[kb] = ac_mma<T>(kf[kb][kk], qf[kk], st[kb]);
-            request();
-            asm volatile("; next rows" ::: "memory");
             if (masked) {
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
@@ -906,7 +961,10 @@ __global__ __launch_bounds__(CW_WAVES * 64) void cache_weigh_kernel(AttendCacheA
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[kb][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][e], a.scale2, -ref));
             }
+            wait_lds();
+            s = s + 1 == SLOTS ? 0 : s + 1;
         }
+        wait_loads<0>();                                // nothing is on its way where the next head's keys will lie
     }
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -1069,18 +1127,18 @@ static size_t attend_cache_ws_bytes(const d3tom_paged_cache& c, int rows, int ma
 template <typename T, int DH>
 static int attend_cache_launch(const AttendCacheArgs& a, int kernel, hipStream_t st) {
     static PerDeviceOnce once;
-    constexpr int WAVES_LDS = 4 * AcTile<T, DH>::WAVE_LDS, ROWS_LDS = AcShared<T, DH>::LDS, WIDE = AcTile<T, DH>::KS > 4 ? 1 : 2;        // (float32 heads of 128 have no registers for 128 rows)
+    constexpr int Q_LDS = 16 * AcTile<T, DH>::ROWB, WAVES_LDS = 4 * AcTile<T, DH>::WAVE_LDS, ROWS_LDS = AcShared<T, DH>::LDS, WIDE = AcTile<T, DH>::KS > 4 ? 1 : 2;        // (float32 heads of 128 have no registers for 128 rows)
     if (!once.run([] {
-            return raise_dynamic_lds(attend_cache_kernel<T, DH, 4>, WAVES_LDS) && raise_dynamic_lds(attend_cache_kernel<T, DH, 2>, WAVES_LDS / 2) &&
-                raise_dynamic_lds(attend_cache_kernel<T, DH, 1>, WAVES_LDS / 4) && raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 1>, ROWS_LDS) &&
+            return raise_dynamic_lds(attend_cache_kernel<T, DH, 4>, WAVES_LDS + Q_LDS) && raise_dynamic_lds(attend_cache_kernel<T, DH, 2>, WAVES_LDS / 2 + Q_LDS) &&
+                raise_dynamic_lds(attend_cache_kernel<T, DH, 1>, WAVES_LDS / 4 + Q_LDS) && raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 1>, ROWS_LDS) &&
                    raise_dynamic_lds(attend_cache_rows_kernel<T, DH, WIDE>, ROWS_LDS);
         })) return D3TOM_ERR_DEVICE;
     const int wgs = (a.nB * a.cache.Hkv * a.S + 7) / 8 * 8 * a.tiles;
     const int W = getenv("AC_W") ? atoi(getenv("AC_W")) : 4;
     if (kernel == AC_WAVES) {
-        if (W == 4) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 4><<<wgs, 256, WAVES_LDS, st>>>(a)));
-        else if (W == 2) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 2><<<wgs, 128, WAVES_LDS / 2, st>>>(a)));
-        else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 1><<<wgs, 64, WAVES_LDS / 4, st>>>(a)));
+        if (W == 4) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 4><<<wgs, 256, WAVES_LDS + Q_LDS, st>>>(a)));
+        else if (W == 2) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 2><<<wgs, 128, WAVES_LDS / 2 + Q_LDS, st>>>(a)));
+        else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 1><<<wgs, 64, WAVES_LDS / 4 + Q_LDS, st>>>(a)));
     }
     else if (kernel == AC_ROWS64) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, 1><<<wgs, 512, ROWS_LDS, st>>>(a)));
     else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, WIDE><<<wgs, 512, ROWS_LDS, st>>>(a)));
@@ -1094,9 +1152,11 @@ static int join_groups(int S, int dh, int threads) {
 }
 template <typename T, int DH>
 static int cache_weigh_launch(const AttendCacheArgs& a, hipStream_t st) {
-    constexpr int KEYS = cw_blocks(AcTile<T, DH>::KS) * 16;
-    const dim3 grid((a.max_len + KEYS - 1) / KEYS, a.nB);
-    D3TOM_LAUNCH(CACHE_WEIGH, st, (cache_weigh_kernel<T, DH><<<grid, CW_WAVES * 64, 0, st>>>(a)));
+    static PerDeviceOnce once;
+    using W = CwTile<T, DH>;
+    if (!once.run([] { return raise_dynamic_lds(cache_weigh_kernel<T, DH>, W::LDS); })) return D3TOM_ERR_DEVICE;
+    const dim3 grid((a.max_len + W::KEYS - 1) / W::KEYS, a.nB);
+    D3TOM_LAUNCH(CACHE_WEIGH, st, (cache_weigh_kernel<T, DH><<<grid, CW_WAVES * 64, W::LDS, st>>>(a)));
     return D3TOM_OK;
 }
 static int attend_cache_check(const d3tom_paged_cache* c, int rows, int max_q, int max_len, int H) {
@@ -1124,6 +1184,7 @@ extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_p
     if (rc != D3TOM_OK) return rc;
     const int dt = cache->dt, dh = cache->dh;
     if ((rc = rows_check(q, q_stride, H, dh, dt)) != D3TOM_OK || (rc = rows_check(o, (int64_t)H * dh, H, dh, dt)) != D3TOM_OK) return rc;
+    if (q_stride * elem_bytes(dt) > (1 << 24)) return D3TOM_ERR_UNSUPPORTED;        // 128 rows apart is a 32-bit offset
     if (!q_off || !ws || !(scale > 0.f) || !(scale < 3.0e38f)) return D3TOM_ERR_INVALID_ARG;
     if ((weight_in && !weight_out) || (weight_out && weight_stride < max_len)) return D3TOM_ERR_INVALID_ARG;
     const AttendCachePlan p = attend_cache_plan(*cache, rows, max_q, max_len, H, weight_out != nullptr);

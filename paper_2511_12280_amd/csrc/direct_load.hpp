@@ -26,6 +26,10 @@ __device__ __forceinline__ void direct_load_16(__amdgpu_buffer_rsrc_t rsrc, int 
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen offset:%3 lds"
                  :: "s"(lds_base - OFFSET), "v"(voff), "s"(rsrc), "n"(OFFSET) : "memory", "m0");
 }
+// The same with 4 bytes a lane, lane i to lds_base + 4 i.
+__device__ __forceinline__ void direct_load_4(__amdgpu_buffer_rsrc_t rsrc, int voff, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds_base), "v"(voff), "s"(rsrc) : "memory", "m0");
+}
 #endif
 
 template <int N>

@@ -177,6 +177,7 @@ def test_attend_cache_refuses(B):
     for rows, most, max_len, H in [(0, 1, 1, 4), (5, 6, 1, 4), (5, 1, 321, 4), (5, 1, 0, 4), (5, 1, 1, 5)]:
         assert B._lib.d3tom_attend_cache_workspace_bytes(_cache(B), rows, most, max_len, H, 0) == 0
     assert _attend(lib, B, cache=_cache(B, B=65535), rows=1 << 30, most=1 << 30) == UNSUPPORTED
+    assert _attend(lib, B, qs=(1 << 23) + 8) == UNSUPPORTED
 
 
 def test_attend_cache_workspace_serves_smaller_calls(B):
