@@ -484,18 +484,13 @@ def d3tom_stack_step_batch(x: torch.Tensor, N: Sequence[int], H: int, F: int, bl
 
 
 # ---- the key/value cache in pages -----------------------------------------------------------------------------
-def _stream_of(t: torch.Tensor, stream):
-    """The stream of a call on t's device.  Work of one device on another's stream would not be ordered with anything."""
-    dev = t.get_device()
-    if (torch._C._cuda_getDevice() if stream is None else stream.device_index) != dev:
-        raise ValueError(f"the tensors lie on device {dev}, the call's stream does not")
-    return _stream(stream)
-
-
-def _on(dev: int, *tensors) -> None:
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError("the tensors of a call lie on different devices")
+def _on(stream):
+    """A call's stream and its device; tensors of another device are refused (work of one device on another's stream would not be
+    ordered with anything).  Sizes, types and devices of the tensors are checked where they are read, csrc/native.cpp: ValueError."""
+    if stream is not None:
+        return stream.cuda_stream, stream.device_index
+    device = torch._C._cuda_getDevice()
+    return torch._C._cuda_getCurrentRawStream(device), device
 
 
 class PagedCache:
@@ -508,7 +503,8 @@ class PagedCache:
         self.k_pages, self.v_pages, self.page_table, self.kv_len = k_pages, v_pages, page_table, kv_len
         self.num_pages, self.page_size, self.Hkv, self.dh = k_pages.shape
         self.B, self.dt, self.dtype, self.device_index = kv_len.numel(), _dt(k_pages), k_pages.dtype, k_pages.get_device()
-        _on(self.device_index, v_pages, page_table, kv_len)
+        if any(t.get_device() != self.device_index for t in (v_pages, page_table, kv_len)):
+            raise ValueError("the tensors of a cache lie on different devices")
         self.struct = _PagedCacheStruct(_ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(kv_len), self.num_pages, self.page_size,
                                         page_table.shape[1], self.B, self.Hkv, self.dh, self.dt)
 
@@ -518,26 +514,14 @@ class Axes:
 
     def __init__(self, pos: torch.Tensor, pairs: Sequence[int], theta: float, ladder: int = D3TOM_AXES_SHARED):
         assert pos.dtype == torch.int32 and pos.dim() == 2 and 1 <= pos.shape[1] == len(pairs) <= D3TOM_MAX_AXES
-        self.pos, self.rows = pos, pos.shape[0]
+        self.pos, self.rows, self.device_index = pos, pos.shape[0], pos.get_device()
         self.struct = _AxesStruct(_ptr(pos), len(pairs), (ctypes.c_int32 * D3TOM_MAX_AXES)(*[int(v) for v in pairs]), int(ladder), float(theta))
 
 
 def d3tom_rope_axes(q: Optional[torch.Tensor], k: Optional[torch.Tensor], axes: Axes, q_out: Optional[torch.Tensor] = None,
                     k_out: Optional[torch.Tensor] = None, stream=None) -> None:
     """q [rows, H, dh], k [rows, Hkv, dh] (rows may lie apart; one may be None); q_out, k_out contiguous (written)."""
-    t = q if q is not None else k
-    rows, _, dh = t.shape
-    assert axes.rows >= rows
-    H = Hkv = 1
-    if q is not None:
-        H = q.shape[1]
-        assert q_out.shape == q.shape and q_out.dtype == q.dtype
-    if k is not None:
-        Hkv = k.shape[1]
-        assert k.shape[0] == rows and k.shape[2] == dh and k.dtype == t.dtype and k_out.shape == k.shape and k_out.dtype == k.dtype
-    _on(t.get_device(), k, q_out, k_out, axes.pos)
-    _check(_native.d3tom_rope_axes(q, k, _dt(t), rows, H, Hkv, dh, axes.struct, q_out if q is not None else None, k_out if k is not None else None,
-                                   _stream_of(t, stream)), "d3tom_rope_axes")
+    _check(_native.d3tom_rope_axes(q, k, axes.struct, axes.rows, axes.device_index, q_out, k_out, *_on(stream)), "d3tom_rope_axes")
 
 
 def d3tom_cache_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, new_off: torch.Tensor, max_new: int, axes: Optional[Axes] = None,
@@ -545,24 +529,9 @@ def d3tom_cache_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, new_
                        slot_token: Optional[torch.Tensor] = None, slot_weight: Optional[torch.Tensor] = None, stream=None) -> None:
     """k, v [rows, Hkv, dh] and q [rows, H, dh] (rows may lie apart); new_off int32 [B + 1]; tokens int32 [rows]; slot_token int32 and
     slot_weight float32 [B, slots] (written)."""
-    rows = k.shape[0]
-    assert k.shape[1:] == (cache.Hkv, cache.dh) and v.shape == k.shape and k.dtype == v.dtype == cache.dtype
-    assert new_off.dtype == torch.int32 and new_off.numel() == cache.B + 1
-    assert axes is None or axes.rows >= rows
-    H = 1
-    if q is not None:
-        H = q.shape[1]
-        assert q.shape[0] == rows and q.shape[2] == cache.dh and q.dtype == cache.dtype and q_out.shape == q.shape and q_out.dtype == q.dtype
-    assert tokens is None or (tokens.dtype == torch.int32 and tokens.numel() >= rows)
-    stride = 0
-    for t, dtype in ((slot_token, torch.int32), (slot_weight, torch.float32)):
-        if t is not None:
-            assert t.dtype == dtype and t.dim() == 2 and t.shape[0] == cache.B and stride in (0, t.shape[1])
-            stride = t.shape[1]
-    _on(cache.device_index, k, v, new_off, q, q_out, tokens, slot_token, slot_weight, axes.pos if axes is not None else None)
-    _check(_native.d3tom_cache_append(cache.struct, k, v, new_off, rows, int(max_new), axes.struct if axes is not None else None, q, H,
-                                      q_out if q is not None else None, tokens, slot_token, slot_weight, stride, _stream_of(k, stream)),
-           "d3tom_cache_append")
+    struct, pos_rows, pos_device = (axes.struct, axes.rows, axes.device_index) if axes is not None else (None, 0, 0)
+    _check(_native.d3tom_cache_append(cache.struct, cache.device_index, k, v, new_off, max_new, struct, pos_rows, pos_device, q, q_out, tokens, slot_token,
+                                      slot_weight, *_on(stream)), "d3tom_cache_append")
 
 
 def d3tom_attend_cache_workspace_bytes(cache: PagedCache, rows: int, max_q: int, max_len: int, H: int, weighed: bool = False) -> int:
@@ -574,17 +543,8 @@ def d3tom_attend_cache(q: torch.Tensor, cache: PagedCache, q_off: torch.Tensor, 
                        weight_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """q [rows, H, dh] (rows may lie apart), q_off int32 [B + 1]; o [rows, H, dh], lse float32 [rows, H], weight_out float32
     [B, slots] (written); weight_in as weight_out."""
-    rows, H, dh = q.shape
-    assert dh == cache.dh and q.dtype == o.dtype == cache.dtype and o.shape == q.shape and q_off.dtype == torch.int32 and q_off.numel() == cache.B + 1
-    assert lse is None or (lse.dtype == torch.float32 and lse.numel() >= rows * H)
-    stride = 0
-    if weight_out is not None:
-        assert weight_out.dtype == torch.float32 and weight_out.dim() == 2 and weight_out.shape[0] == cache.B
-        assert weight_in is None or (weight_in.dtype == torch.float32 and weight_in.shape == weight_out.shape)
-        stride = weight_out.shape[1]
-    _on(cache.device_index, q, q_off, o, ws, lse, weight_in, weight_out)
-    _check(_native.d3tom_attend_cache(q, cache.struct, q_off, rows, int(max_q), int(max_len), H, float(scale), int(causal), o, lse, weight_in,
-                                      weight_out, stride, ws, ws.numel() * ws.element_size(), _stream_of(q, stream)), "d3tom_attend_cache")
+    _check(_native.d3tom_attend_cache(q, cache.struct, cache.device_index, q_off, max_q, max_len, scale, causal, o, lse, weight_in, weight_out, ws,
+                                      *_on(stream)), "d3tom_attend_cache")
     return o
 
 
@@ -596,14 +556,8 @@ def d3tom_cache_evict(cache: PagedCache, max_len: int, keep: torch.Tensor, first
                       token_in: torch.Tensor, weight_out: torch.Tensor, token_out: torch.Tensor, len_out: torch.Tensor, ws: torch.Tensor,
                       src: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """keep, len_out int32 [B]; weight_* float32 and token_*, src int32 [B, slots]; the cache's rows move in place.  Returns len_out."""
-    shape = weight_in.shape
-    assert weight_in.dtype == weight_out.dtype == torch.float32 and token_in.dtype == token_out.dtype == torch.int32
-    assert len(shape) == 2 and shape[0] == cache.B and weight_out.shape == token_in.shape == token_out.shape == shape
-    assert src is None or (src.dtype == torch.int32 and src.shape == shape)
-    assert keep.dtype == len_out.dtype == torch.int32 and keep.numel() == len_out.numel() == cache.B
-    _on(cache.device_index, keep, weight_in, token_in, weight_out, token_out, len_out, ws, src)
-    _check(_native.d3tom_cache_evict(cache.struct, int(max_len), keep, int(first), int(recent), weight_in, token_in, weight_out, token_out,
-                                     shape[1], len_out, src, ws, ws.numel() * ws.element_size(), _stream_of(keep, stream)), "d3tom_cache_evict")
+    _check(_native.d3tom_cache_evict(cache.struct, cache.device_index, max_len, keep, first, recent, weight_in, token_in, weight_out, token_out, len_out, ws, src,
+                                     *_on(stream)), "d3tom_cache_evict")
     return len_out
 
 

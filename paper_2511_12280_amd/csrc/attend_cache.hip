@@ -6,7 +6,6 @@
 // What the slots got (weight_out) is formed from the joined sums behind that: p = 2^(logit - lse).
 #include "cache.hpp"
 #include "direct_load.hpp"
-#include <stdlib.h>
 
 namespace d3tom {
 
@@ -17,6 +16,7 @@ struct AttendCacheArgs {
     const int32_t* q_off;
     int nB, rows, max_q, max_len, H, G, causal; // G: query heads of a key head
     float scale2;                               // scale * log2(e)
+    float per_G, per_heads, per_Hkv;            // 1 / G, 1 / (nB Hkv), 1 / Hkv
     int S, run;                                 // runs of a cache, slots of a run
     void* o;
     float *lse, *lse2;                          // natural logarithm (the caller's), base 2 (for the weights)
@@ -28,6 +28,15 @@ struct AttendCacheArgs {
     float* weight_out;
     int weight_stride;
 };
+
+// x / d of numbers below 2^24, `per` = 1 / d: the float quotient is less than one off.  (The integer division is 40 instructions, and a kernel has a handful of
+// them in front of its first load.)
+__device__ __forceinline__ int div_by(int x, int d, float per) {
+    int q = (int)((float)x * per);
+    q -= q * d > x ? 1 : 0;
+    q += (q + 1) * d <= x ? 1 : 0;
+    return q;
+}
 
 // A sample's rows: first one, how many.  Offsets that do not fit are cut to what there is.
 __device__ __forceinline__ int sample_rows(const AttendCacheArgs& a, int b, int& r0) {
@@ -232,7 +241,8 @@ __device__ __forceinline__ void ac_softmax(f32x4 (&st)[KB], f32x4 (&o)[DB], floa
 #endif
 }
 
-template <typename T, int DH, int WAVES>
+constexpr int WAVES = 4;
+template <typename T, int DH>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCacheArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = AcTile<T, DH>;
@@ -245,10 +255,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
     int id = blockIdx.x;
     const int xcd = id & 7;
     id >>= 3;
-    const int tile = id % a.tiles;
-    int unit = (id / a.tiles) * 8 + xcd;
-    const int heads = a.nB * a.cache.Hkv, s = unit / heads; unit -= s * heads;
-    const int kvh = unit % a.cache.Hkv, b = unit / a.cache.Hkv;
+    int tile = 0;
+    if (a.tiles > 1) { tile = id % a.tiles; id /= a.tiles; }
+    int unit = id * 8 + xcd;
+    const int heads = a.nB * a.cache.Hkv, s = __builtin_amdgcn_readfirstlane(div_by(unit, heads, a.per_heads));
+    unit -= s * heads;
+    const int b = __builtin_amdgcn_readfirstlane(div_by(unit, a.cache.Hkv, a.per_Hkv)), kvh = unit - b * a.cache.Hkv;
     if (s >= a.S) return;
     // Pages of this wave's blocks of 16 slots: lane i has that of block i % KB of its tile i / KB.  Requested with the sample's sizes, not behind them: what lies
     // behind its last page is never used.
@@ -260,12 +272,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
     if (R0 >= R) return;
     const int n = a.cache.length(b, a.max_len);
     const int last = min(R0 + 15, R - 1);
-    const int j1 = min(row_limit(a, n, nq, last / a.G), j0 + a.run);
+    const int j1 = min(row_limit(a, n, nq, div_by(last, a.G, a.per_G)), j0 + a.run);
     if (j0 >= j1 && s > 0) return;
-    const int x = min(R0 + r, R - 1), xi = x / a.G, xh = kvh * a.G + (x - xi * a.G);          // this lane's column
+    const int x = min(R0 + r, R - 1), xi = div_by(x, a.G, a.per_G), xh = kvh * a.G + (x - xi * a.G);          // this lane's column
     const size_t row = (size_t)(r0 + xi);
     const int limit = min(row_limit(a, n, nq, xi), j1);
-    const int limit0 = min(row_limit(a, n, nq, R0 / a.G), j1);                                 // slots that all columns see
+    const int limit0 = min(row_limit(a, n, nq, div_by(R0, a.G, a.per_G)), j1);                                 // slots that all columns see
 
     const int ntile = j1 > j0 ? (j1 - j0 + KEYS - 1) / KEYS : 0;
     const int mine = (ntile - wave + WAVES - 1) / WAVES;                                       // tiles wave, wave + WAVES, ...
@@ -283,13 +295,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
     const uint32_t ring0 = (uint32_t)(size_t)(lds_ptr_t)ring + wave * C::WAVE_LDS;
     const char* kbase = static_cast<const char*>(a.k_pages) + (size_t)kvh * ROWB;
     const char* vbase = static_cast<const char*>(a.v_pages) + (size_t)kvh * ROWB;
-    // tile t of this wave: rows past j1 (and tiles that there are not) load as zeros without touching memory
+    // tile t of this wave; rows past j1 load as zeros without touching memory
     auto issue = [&](const char* base, const int (&off)[LDB], int t, uint32_t lds) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             const int slot = j0 + (t * WAVES + wave) * KEYS + kb * 16;
             const uint32_t page = __builtin_amdgcn_readlane(ids, (t * KB + kb) & 63);
-            const int there = t < mine ? min(max(j1 - slot, 0), 16) : 0;
+            const int there = min(max(j1 - slot, 0), 16);
             const __amdgpu_buffer_rsrc_t rs = make_uniform_rsrc(base + a.cache.row(page, slot) * row_bytes, there ? (uint32_t)(there - 1) * row_bytes + ROWB : 0u);
 #pragma unroll
             for (int i = 0; i < LDB; ++i) direct_load_16(rs, off[i], lds + (kb * LDB + i) * 1024);
@@ -301,16 +313,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
     // bytes of a row at a time, they are slower than the keys, and these waited for them: 1 us.)
     const uint32_t q_lds = (uint32_t)(size_t)(lds_ptr_t)ring + WAVES * C::WAVE_LDS;
     constexpr int QLD = 16 / RPI;
-    const __amdgpu_buffer_rsrc_t rq = make_uniform_rsrc(static_cast<const char*>(a.q) + ((size_t)(r0 + R0 / a.G) * a.q_stride + (size_t)kvh * a.G * DH) * sizeof(T), ~0u);
+    const __amdgpu_buffer_rsrc_t rq = make_uniform_rsrc(static_cast<const char*>(a.q) + ((size_t)(r0 + div_by(R0, a.G, a.per_G)) * a.q_stride + (size_t)kvh * a.G * DH) * sizeof(T), ~0u);
 #pragma unroll
     for (int i = 0; i < (QLD + WAVES - 1) / WAVES; ++i) {
         const int li = i * WAVES + wave;
         if (QLD % WAVES == 0 || li < QLD) {
-            const int x2 = li * RPI + ld_row, X = min(R0 + x2, R - 1), Xi = X / a.G;
-            direct_load_16(rq, (uint32_t)((Xi - R0 / a.G) * (int)a.q_stride + (X - Xi * a.G) * DH) * sizeof(T) + ((ld_pos ^ C::k_turn(x2)) << 4), q_lds + li * 1024);
+            const int x2 = li * RPI + ld_row, X = min(R0 + x2, R - 1), Xi = div_by(X, a.G, a.per_G);
+            direct_load_16(rq, (uint32_t)((Xi - div_by(R0, a.G, a.per_G)) * (int)a.q_stride + (X - Xi * a.G) * DH) * sizeof(T) + ((ld_pos ^ C::k_turn(x2)) << 4), q_lds + li * 1024);
         }
     }
-    issue_k(0); issue_v(0); issue_k(1); issue_v(1);
+    if (mine > 0) { issue_k(0); issue_v(0); }
+    if (mine > 1) { issue_k(1); issue_v(1); }
 
     int k_addr[KS], v_addr[DB];
 #pragma unroll
@@ -328,7 +341,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
 #pragma unroll
     for (int t = 0; t < DB; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    wait_loads_and_barrier<4 * C::LD>();                       // the queries are there
+    if (mine > 1) wait_loads<4 * C::LD>();             // the queries are there
+    else if (mine > 0) wait_loads<2 * C::LD>();
+    else wait_loads<0>();
+    wait_loads_and_barrier<63>();
     uint4 qf[KS];
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const uint4*>(ring + WAVES * C::WAVE_LDS + k_addr[kk]);
@@ -338,7 +354,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
     for (int t = 0; t < mine; ++t) {
         const char* w = ring + wave * C::WAVE_LDS + (t & 1) * C::STAGE;
         const int key0 = j0 + (t * WAVES + wave) * KEYS;
-        wait_loads<3 * C::LD>();                           // K of this tile is there
+        if (t + 1 < mine) wait_loads<3 * C::LD>();         // K of this tile is there
+        else wait_loads<C::LD>();
         f32x4 st[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
@@ -347,14 +364,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
             for (int kk = 0; kk < KS; ++kk) st[kb] = ac_mma<T>(*reinterpret_cast<const uint4*>(w + k_addr[kk] + kb * 16 * ROWB), qf[kk], st[kb]);
         }
         wait_lds();
-        issue_k(t + 2);
+        if (t + 2 < mine) issue_k(t + 2);
         if (kept && real) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
                 if (key0 + kb * 16 < j1) *reinterpret_cast<f32x4*>(kept + key0 + kb * 16 + 4 * g) = f32x4{st[kb][0] * a.scale2, st[kb][1] * a.scale2, st[kb][2] * a.scale2, st[kb][3] * a.scale2};
         }
         ac_softmax<KB, DB>(st, o, m, l, a.scale2, key0 + KEYS > limit0, limit - key0 - 4 * g);
-        wait_loads<3 * C::LD>();                           // V of this tile
+        if (t + 2 < mine) wait_loads<3 * C::LD>();         // V of this tile
+        else if (t + 1 < mine) wait_loads<2 * C::LD>();
+        else wait_loads<0>();
         if constexpr (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) ac_short4* tr_ptr;
 #pragma unroll
@@ -380,7 +399,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
                         o[t2] = __builtin_amdgcn_mfma_f32_16x16x4f32(*reinterpret_cast<const float*>(w + v_addr[t2] + (kb * 16 + e) * ROWB), st[kb][e], o[t2], 0, 0, 0);
         }
         wait_lds();
-        issue_v(t + 2);
+        if (t + 2 < mine) issue_v(t + 2);
     }
     wait_loads_and_barrier<0>();                           // nothing is on its way into the rings any more
     // the waves' parts, rows of queries
@@ -395,7 +414,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
     constexpr int TPR = 4 * WAVES, CH = DH / TPR;
     const int y = tid / TPR, Y = R0 + y;
     if (Y >= R) return;
-    const int yi = Y / a.G, yh = kvh * a.G + (Y - yi * a.G);
+    const int yi = div_by(Y, a.G, a.per_G), yh = kvh * a.G + (Y - yi * a.G);
     float mt = -INFINITY;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) mt = fmaxf(mt, part_m[w][y]);
@@ -461,10 +480,12 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
     int id = blockIdx.x;
     const int xcd = id & 7;
     id >>= 3;
-    const int tile = id % a.tiles;
-    int unit = (id / a.tiles) * 8 + xcd;
-    const int heads = a.nB * a.cache.Hkv, s = unit / heads; unit -= s * heads;
-    const int kvh = unit % a.cache.Hkv, b = unit / a.cache.Hkv;
+    int tile = 0;
+    if (a.tiles > 1) { tile = id % a.tiles; id /= a.tiles; }
+    int unit = id * 8 + xcd;
+    const int heads = a.nB * a.cache.Hkv, s = __builtin_amdgcn_readfirstlane(div_by(unit, heads, a.per_heads));
+    unit -= s * heads;
+    const int b = __builtin_amdgcn_readfirstlane(div_by(unit, a.cache.Hkv, a.per_Hkv)), kvh = unit - b * a.cache.Hkv;
     if (s >= a.S) return;
     const int j0 = s * a.run, my_page = a.cache.page_of(b, min(j0 + (tid & (W::PAGES - 1)) * 16, a.last_slot));         // (see above)
     int r0;
@@ -473,7 +494,7 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
     const int R = nq * a.G, R0 = tile * ROWS;
     if (R0 >= R) return;
     const int n = a.cache.length(b, a.max_len);
-    const int j1 = min(row_limit(a, n, nq, (min(R0 + ROWS, R) - 1) / a.G), j0 + a.run);
+    const int j1 = min(row_limit(a, n, nq, div_by(min(R0 + ROWS, R) - 1, a.G, a.per_G)), j0 + a.run);
     if (j0 >= j1 && s > 0) return;
     const int W0 = R0 + rg * 16 * QB;                  // this wave's first row
     const bool works = W0 < R;
@@ -481,12 +502,12 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
     int xh[QB], limit[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const int x = min(W0 + qb * 16 + r, R - 1), xi = x / a.G;
+        const int x = min(W0 + qb * 16 + r, R - 1), xi = div_by(x, a.G, a.per_G);
         xh[qb] = kvh * a.G + (x - xi * a.G);
         row[qb] = (size_t)(r0 + xi);
         limit[qb] = min(row_limit(a, n, nq, xi), j1);
     }
-    const int limit0 = min(row_limit(a, n, nq, min(W0, R - 1) / a.G), j1);
+    const int limit0 = min(row_limit(a, n, nq, div_by(min(W0, R - 1), a.G, a.per_G)), j1);
     const int ntile = j1 > j0 ? (j1 - j0 + KEYS - 1) / KEYS : 0;
     if (tid < W::PAGES) pages[tid] = a.cache.readable(my_page);
     const uint32_t row_bytes = (uint32_t)a.cache.row_elems() * sizeof(T);
@@ -519,18 +540,20 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
     // the queries lie where tiles 2 and 3 will
     constexpr int QLD = ROWS / RPI / 8;
     {
-        const __amdgpu_buffer_rsrc_t rq = make_uniform_rsrc(static_cast<const char*>(a.q) + ((size_t)(r0 + R0 / a.G) * a.q_stride + (size_t)kvh * a.G * DH) * sizeof(T), ~0u);
+        const __amdgpu_buffer_rsrc_t rq = make_uniform_rsrc(static_cast<const char*>(a.q) + ((size_t)(r0 + div_by(R0, a.G, a.per_G)) * a.q_stride + (size_t)kvh * a.G * DH) * sizeof(T), ~0u);
 #pragma unroll
         for (int i = 0; i < QLD; ++i) {
-            const int x = (wave * QLD + i) * RPI + ld_row, X = min(R0 + x, R - 1), Xi = X / a.G;
-            direct_load_16(rq, (uint32_t)((Xi - R0 / a.G) * (int)a.q_stride + (X - Xi * a.G) * DH) * sizeof(T) + ((ld_pos ^ C::k_turn(x & 15)) << 4),
+            const int x = (wave * QLD + i) * RPI + ld_row, X = min(R0 + x, R - 1), Xi = div_by(X, a.G, a.per_G);
+            direct_load_16(rq, (uint32_t)((Xi - div_by(R0, a.G, a.per_G)) * (int)a.q_stride + (X - Xi * a.G) * DH) * sizeof(T) + ((ld_pos ^ C::k_turn(x & 15)) << 4),
                            ring0 + 2 * W::STAGE + (wave * QLD + i) * 1024);
         }
     }
     __syncthreads();
-    issue(0, pages_of(0));
-    issue(1, pages_of(1));
-    wait_loads_and_barrier<2 * 2 * LD>();              // the queries are there
+    if (ntile > 0) issue(0, pages_of(0));
+    if (ntile > 1) issue(1, pages_of(1));
+    if (ntile > 1) wait_loads_and_barrier<2 * 2 * LD>();       // the queries are there
+    else if (ntile > 0) wait_loads_and_barrier<2 * LD>();
+    else wait_loads_and_barrier<0>();
     uint4 qf[QB][KS];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
@@ -638,8 +661,9 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
     // and matrix units in turn.  (The tile before is then still read: two are on their way.)  Every wave comes to every barrier.
     uint32_t ids = pages_of(2);
     auto meet = [&](int t) {                           // tile t is there, tile t - 2 is done with
-        wait_loads_and_barrier<2 * LD>();
-        issue(t + 2, ids);
+        if (t + 1 < ntile) wait_loads_and_barrier<2 * LD>();
+        else wait_loads_and_barrier<0>();
+        if (t + 2 < ntile) issue(t + 2, ids);
         ids = pages_of(t + 3);
     };
     if (ntile > 0) meet(0);
@@ -894,14 +918,14 @@ __global__ __launch_bounds__(CW_WAVES * 64, 2) void cache_weigh_kernel(AttendCac
             for (int kk = 0; kk < KS; ++kk) kf[kb][kk] = *reinterpret_cast<const uint4*>(at + kb * 16 * ROWB + q_addr[kk]);
         wait_lds();
         // The block that is requested next: its first row, and (row, head) of this lane's rows in the loads and of its column, all moving on together.
-        int x0 = first, i0 = first / a.G, li[LDB], lx[LDB], ci, cx;
+        int x0 = first, i0 = div_by(first, a.G, a.per_G), li[LDB], lx[LDB], ci, cx;
 #pragma unroll
         for (int i = 0; i < LDB; ++i) {
             const int x = first + i * RPI + ld_row;
-            li[i] = x / a.G;
+            li[i] = div_by(x, a.G, a.per_G);
             lx[i] = x - li[i] * a.G;
         }
-        ci = (first + r) / a.G;
+        ci = div_by(first + r, a.G, a.per_G);
         cx = first + r - ci * a.G;
         int rest = first - i0 * a.G;
         int seen_i = ci;                                // row of this lane's column in the block that is used next
@@ -1074,8 +1098,10 @@ __global__ __launch_bounds__(256) void cache_weigh_generic_kernel(AttendCacheArg
 }
 
 // How a call goes: a rule on host-known sizes only.
-//   heads of 64 and 128   up to 16 rows to a key head: waves on their own, a run for every compute unit
-//                         more: 64 or 128 rows that share tiles, two workgroups to a unit
+//   heads of 64 and 128   up to 16 rows to a key head: waves on their own; more: 64 or 128 rows that share tiles.  A run for every compute unit: more runs cost a round of
+//                         workgroups each (32 samples of 2048 slots, 8 key heads of 128 in one, two, four rounds 49, 54, 57 us), fewer leave units idle (8 samples 17.3
+//                         and 16.2 us with 128 and 256).  One run, without the joining, where a head's K is short: one sample, 8 heads of 128, 512, 768 and
+//                         1024 slots 7.2, 8.7 and 10.4 us against 9.9, 9.9 and 9.8 in runs of 256; float32 heads of 64, 256 and 512 slots 7.1 and 10.6 against 9.8 and 10.0.
 //   others                a workgroup per row, head and run
 enum { AC_GENERIC = 0, AC_WAVES, AC_ROWS64, AC_ROWS128 };
 struct AttendCachePlan {
@@ -1092,15 +1118,12 @@ static AttendCachePlan attend_cache_plan(const d3tom_paged_cache& c, int rows, i
     const int tile_rows[] = {1, 16, 64, 128}, want[] = {1024, 256, 256, 256};
     p.tiles = (int)((R + tile_rows[p.kernel] - 1) / tile_rows[p.kernel]);
     const long long groups = (long long)c.B * (p.kernel == AC_GENERIC ? (long long)max_q * H : (long long)c.Hkv * p.tiles), step = p.kernel == AC_GENERIC ? 256 : 128;
-    int wantk = want[p.kernel]; if (getenv("AC_WANT")) wantk = atoi(getenv("AC_WANT"));
-    long long S = groups >= wantk ? 1 : wantk / groups;
+    long long S = groups >= want[p.kernel] ? 1 : want[p.kernel] / groups;
     const long long most = (max_len + step - 1) / step;
     S = S > most ? most : S;
-    if (p.kernel == AC_WAVES && (size_t)max_len * c.dh * elem_bytes(c.dt) <= (getenv("AC_ONE") ? atoi(getenv("AC_ONE")) : 128) * 1024) S = 1;
+    if (p.kernel == AC_WAVES && (size_t)max_len * c.dh * elem_bytes(c.dt) <= (c.dt == D3TOM_BF16 ? 192u : 96u) * 1024) S = 1;
     p.run = (int)((most + S - 1) / S * step);
-    if (getenv("AC_RUN")) p.run = atoi(getenv("AC_RUN"));
-    const int maxrun = p.kernel == AC_WAVES && getenv("AC_W") ? 1024 * atoi(getenv("AC_W")) : AC_MAX_RUN;
-    if (p.kernel != AC_GENERIC && p.run > maxrun) p.run = maxrun;
+    if (p.kernel != AC_GENERIC && p.run > AC_MAX_RUN) p.run = AC_MAX_RUN;
     p.S = (max_len + p.run - 1) / p.run;
     p.keep = weighed && p.kernel == AC_WAVES;
     p.lpad = (max_len + 15) / 16 * 16;
@@ -1127,19 +1150,15 @@ static size_t attend_cache_ws_bytes(const d3tom_paged_cache& c, int rows, int ma
 template <typename T, int DH>
 static int attend_cache_launch(const AttendCacheArgs& a, int kernel, hipStream_t st) {
     static PerDeviceOnce once;
-    constexpr int Q_LDS = 16 * AcTile<T, DH>::ROWB, WAVES_LDS = 4 * AcTile<T, DH>::WAVE_LDS, ROWS_LDS = AcShared<T, DH>::LDS, WIDE = AcTile<T, DH>::KS > 4 ? 1 : 2;        // (float32 heads of 128 have no registers for 128 rows)
+    using C = AcTile<T, DH>;
+    constexpr int WAVES_LDS = WAVES * C::WAVE_LDS + 16 * C::ROWB, ROWS_LDS = AcShared<T, DH>::LDS;
+    constexpr int WIDE = C::KS > 4 ? 1 : 2;     // (float32 heads of 128 have no registers for 128 rows: the plan gives them 64)
     if (!once.run([] {
-            return raise_dynamic_lds(attend_cache_kernel<T, DH, 4>, WAVES_LDS + Q_LDS) && raise_dynamic_lds(attend_cache_kernel<T, DH, 2>, WAVES_LDS / 2 + Q_LDS) &&
-                raise_dynamic_lds(attend_cache_kernel<T, DH, 1>, WAVES_LDS / 4 + Q_LDS) && raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 1>, ROWS_LDS) &&
+            return raise_dynamic_lds(attend_cache_kernel<T, DH>, WAVES_LDS) && raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 1>, ROWS_LDS) &&
                    raise_dynamic_lds(attend_cache_rows_kernel<T, DH, WIDE>, ROWS_LDS);
         })) return D3TOM_ERR_DEVICE;
     const int wgs = (a.nB * a.cache.Hkv * a.S + 7) / 8 * 8 * a.tiles;
-    const int W = getenv("AC_W") ? atoi(getenv("AC_W")) : 4;
-    if (kernel == AC_WAVES) {
-        if (W == 4) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 4><<<wgs, 256, WAVES_LDS + Q_LDS, st>>>(a)));
-        else if (W == 2) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 2><<<wgs, 128, WAVES_LDS / 2 + Q_LDS, st>>>(a)));
-        else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, 1><<<wgs, 64, WAVES_LDS / 4 + Q_LDS, st>>>(a)));
-    }
+    if (kernel == AC_WAVES) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH><<<wgs, 64 * WAVES, WAVES_LDS, st>>>(a)));
     else if (kernel == AC_ROWS64) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, 1><<<wgs, 512, ROWS_LDS, st>>>(a)));
     else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, WIDE><<<wgs, 512, ROWS_LDS, st>>>(a)));
     return D3TOM_OK;
@@ -1196,6 +1215,7 @@ extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_p
     a.q = q; a.k_pages = cache->k_pages; a.v_pages = cache->v_pages; a.q_stride = q_stride; a.q_off = q_off;
     a.nB = cache->B; a.rows = rows; a.max_q = max_q; a.max_len = max_len; a.H = H; a.G = H / cache->Hkv; a.causal = causal != 0;
     a.scale2 = scale * LOG2E;
+    a.per_G = 1.0f / (float)a.G; a.per_Hkv = 1.0f / (float)cache->Hkv; a.per_heads = 1.0f / ((float)cache->Hkv * (float)cache->B);
     a.last_slot = max_len - 1;                  // (the table has all of max_len)
     a.S = p.S; a.run = p.run; a.o = o; a.lse = lse; a.lpad = p.lpad; a.tiles = p.tiles;
     a.lse2 = weight_out ? (float*)((char*)ws + p.lse2) : nullptr;

@@ -225,10 +225,23 @@ def test_binding_refuses_what_it_cannot_pass_on(B):
     with pytest.raises(ValueError):
         B.Axes(torch.zeros(4, 3, dtype=torch.int32), [10, 12, 10], 10000.0)
     from paper_2511_12280_amd import _native
+    cache, axes, none9 = _cache(B), _axes(B), [None] * 9
     with pytest.raises(ValueError, match="another size"):
-        _native.d3tom_cache_evict(_axes(B), 1, None, 0, 0, None, None, None, None, 1, None, None, None, 0, None)
+        _native.d3tom_cache_evict(axes, 0, 1, None, 0, 0, *none9)
     with pytest.raises(TypeError):
-        _native.d3tom_cache_evict(4096, 1, None, 0, 0, None, None, None, None, 1, None, None, None, 0, None)
-    with pytest.raises(ValueError, match="rows of heads on the GPU"):
-        _native.d3tom_rope_axes(torch.zeros(4, 2, 64), None, 0, 4, 2, 2, 64, _axes(B), None, None, None)
-    assert _native.d3tom_rope_axes(None, None, 0, 4, 2, 2, 64, _axes(B), None, None, None) == INVALID
+        _native.d3tom_cache_evict(4096, 0, 1, None, 0, 0, *none9)
+    with pytest.raises(TypeError):
+        _native.d3tom_cache_evict(cache, 0, 1)
+    with pytest.raises(ValueError, match="a cache is missing"):
+        _native.d3tom_cache_evict(None, 0, 1, None, 0, 0, *none9)
+    with pytest.raises(ValueError, match="a tensor is missing"):
+        _native.d3tom_cache_evict(cache, 0, 1, None, 0, 0, None, None, None, None, None, 17, None, None, 0)
+    host = torch.zeros(4, 2, 64)
+    for bad in (host, host.as_subclass(type("Sub", (torch.Tensor,), {}))):
+        with pytest.raises(ValueError, match="on the GPU"):
+            _native.d3tom_rope_axes(bad, None, axes, 4, 0, None, None, None, 0)
+    with pytest.raises(ValueError, match="keys and values"):
+        _native.d3tom_cache_append(cache, 0, None, None, None, 1, None, 0, 0, *[None] * 6, 0)
+    with pytest.raises(ValueError, match="different devices"):
+        _native.d3tom_attend_cache(None, cache, 0, None, 1, 1, 0.1, 0, *[None] * 6, 0)
+    assert _native.d3tom_rope_axes(None, None, axes, 4, 0, None, None, None, 0) == INVALID

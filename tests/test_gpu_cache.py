@@ -601,3 +601,32 @@ def test_streams_and_devices(B):
         B.d3tom_attend_cache(q, c.handle, off.cpu(), 1, 90, 0.1, False, o2, ws[1])
     with pytest.raises(B.D3tomError):
         B.d3tom_attend_cache(q, c.handle, off, 1, 10 ** 6, 0.1, False, o2, ws[1])
+
+
+def test_bindings_check_shapes_types_and_devices(B):
+    c = Cache(B, [90, 20], 2, 64, 16, "bf16", seed=2)
+    z = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype, device="cuda")
+    q, k, off, pos = z(5, 4, 64), z(5, 2, 64), _i32([0, 4, 5]), z(5, 2, dtype=torch.int32)
+    axes = B.Axes(pos, [16, 16], 10000.0)
+    for kw in (dict(q_out=z(5, 4, 32)), dict(q_out=z(5, 4, 64, dtype=torch.float32)), dict(q_out=None), dict(q_out=z(5, 5, 64)[:, :4]), dict(k=z(4, 2, 64)),
+               dict(k=z(5, 2, 64, dtype=torch.float32)), dict(q=z(5, 64, 4).transpose(1, 2)), dict(q=z(5, 256)), dict(q=z(5, 4, 64).half()), dict(axes=B.Axes(pos[:4].clone(), [16, 16], 10000.0))):
+        with pytest.raises(ValueError):
+            B.d3tom_rope_axes(**dict(dict(q=q, k=k, axes=axes, q_out=z(5, 4, 64), k_out=z(5, 2, 64)), **kw))
+    slot_t, slot_w = z(2, 100, dtype=torch.int32), z(2, 100, dtype=torch.float32)
+    for kw in (dict(k=z(5, 3, 64)), dict(k=z(5, 2, 64, dtype=torch.float32)), dict(v=z(4, 2, 64)), dict(new_off=_i32([0, 5])), dict(new_off=off.float()), dict(tokens=_i32([1, 2])),
+               dict(slot_token=z(3, 100, dtype=torch.int32)), dict(slot_weight=z(2, 99, dtype=torch.float32)), dict(slot_weight=z(2, 100)), dict(q=q, q_out=None, axes=axes),
+               dict(q=q[:4], q_out=q[:4].clone(), axes=axes)):
+        with pytest.raises(ValueError):
+            B.d3tom_cache_append(**dict(dict(cache=c.handle, k=k, v=k, new_off=off, max_new=4, tokens=_i32([0] * 5), slot_token=slot_t, slot_weight=slot_w), **kw))
+    ws = B.workspace(1 << 22)
+    for kw in (dict(q=z(5, 4, 32)), dict(q=q.float()), dict(o=z(4, 4, 64)), dict(o=z(5, 4, 64, dtype=torch.float32)), dict(q_off=_i32([0, 5])), dict(lse=z(5, 3, dtype=torch.float32)),
+               dict(weight_out=z(3, 100, dtype=torch.float32)), dict(weight_in=z(2, 90, dtype=torch.float32)), dict(ws=None)):
+        with pytest.raises(ValueError):
+            B.d3tom_attend_cache(**dict(dict(q=q, cache=c.handle, q_off=off, max_q=4, max_len=90, scale=0.1, causal=False, o=z(5, 4, 64), ws=ws,
+                                             weight_in=slot_w, weight_out=slot_w.clone()), **kw))
+    for kw in (dict(keep=_i32([3])), dict(keep=_i32([3, 4]).long()), dict(weight_in=slot_t), dict(token_in=slot_w), dict(token_out=z(2, 99, dtype=torch.int32)), dict(len_out=_i32([0])),
+               dict(src=z(2, 99, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            B.d3tom_cache_evict(**dict(dict(cache=c.handle, max_len=90, keep=_i32([3, 4]), first=0, recent=0, weight_in=slot_w, token_in=slot_t, weight_out=slot_w.clone(),
+                                            token_out=slot_t.clone(), len_out=_i32([0, 0]), ws=ws), **kw))
+    torch.cuda.synchronize()
