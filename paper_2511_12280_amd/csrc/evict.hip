@@ -1,22 +1,23 @@
 // d3tom_cache_evict: a cache shortened by the attention weight that its slots have got.
 //
 // Order of the slots: an unsigned key per slot, all ones for a protected one, else the order-preserving image of its weight; larger
-// first, equal keys by the slot.  One workgroup per sample finds the k-th largest key by counting: 2048 bins over the range that the keys
-// have (weights are spread over many octaves, and the image is nearly their logarithm, so that the counts do not meet in few bins as they would in bins of a
-// fixed number of leading bits), then over the bin that the key lies in, at most three times.  Counts of integers: the order of the additions does not
-// show.  It leaves a bit for every slot that stays, and for each word of 64 how many holes (slots below k that do not stay) and movers (slots
-// from k on that do) lie in front of it: there are as many of either.
+// first, equal keys by the slot.  The k-th largest key is found by counting: 2048 bins over the range that the keys have (weights are spread over
+// many octaves, and the image is nearly their logarithm, so that the counts do not meet in few bins as they would in bins of a fixed number of leading
+// bits), then twice over the bin that the key lies in.  Counts of integers: the order of the additions does not show.  What is left of it is a
+// bit for every slot that stays, and for each word of 64 how many holes (slots below k that do not stay) and movers (slots from k on that do) lie in front
+// of it: there are as many of either.
 //
-// A second launch has a workgroup for every word below k: it pairs the word's holes with the movers of the same numbers and moves their rows.
-// Every mover lies at k or above and every hole below it, so that the moves need no order among themselves.
+// A sample of one slice of 4096 slots is a single workgroup's, its keys in registers.  Longer caches are cut into slices with a workgroup each, in a launch for every step:
+// what a step needs of all slices is small and read by every workgroup.  (One workgroup for 65521 slots took 72 us at best: a compute unit waits 2 us for a batch of
+// 64 KB, four times eight batches.)
 //
-// The selection has one compute unit per sample; its keys stay in registers up to 16384 slots and are formed again in every turn beyond that.
-// The moves are bound by memory.
+// The last launch has a workgroup for every word below k: it pairs the word's holes with the movers of the same numbers and moves their rows.
+// Every mover lies at k or above and every hole below it, so that the moves need no order among themselves.  Bound by memory.
 #include "cache.hpp"
 
 namespace d3tom {
 
-constexpr int EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64, EV_BINS = 2048;
+constexpr int EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64, EV_BINS = 2048, EV_TURNS = 4, EV_SLICE = EV_THREADS * EV_TURNS, EV_LEVELS = 3;
 
 struct EvictArgs {
     CacheView cache;
@@ -34,6 +35,10 @@ struct EvictArgs {
     unsigned long long* stays;
     int32_t *holes, *movers;
     int words;
+    // of several slices: (largest number, range of the images) and (larger and equal keys below k, from k on) [B, slices]; counts [B, levels, bins]
+    int slices;
+    int4 *ranges, *counts;
+    int32_t* bins;
     char *k_pages, *v_pages;
     int row_bytes;
 };
@@ -64,174 +69,276 @@ __device__ __forceinline__ int ev_reduce(int v, F&& f) {
 #endif
 }
 
-// P: keys of a thread in registers, 64 slots to a wave and turn; 0: any number, formed again each time, EV_BATCH turns requested together
-constexpr int EV_BATCH = 8;
-template <int P>
-__global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __shared__ int hist[EV_BINS];
-    __shared__ int wave_a[EV_WAVES], wave_b[EV_WAVES], wave_c[EV_WAVES];
-    __shared__ uint32_t wave_lo[EV_WAVES], wave_hi[EV_WAVES];
-    __shared__ int s_digit, s_above, s_equal;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
-    const int n = a.cache.length(b, a.max_len);
-    const int k = min(max(a.keep[b], 0), n);
-    if (n == 0) {
-        if (tid == 0) a.sizes[b] = make_int2(0, 0);
-        return;
-    }
-    const float* w = a.weight_in + (size_t)b * a.stride;
-    const int32_t* tok = a.token_in + (size_t)b * a.stride;
-    // A wave has consecutive slots.  Every turn is taken, live or not: loads behind a branch would wait for each other.
-    const int turns = P > 0 ? P : (n + EV_THREADS - 1) / EV_THREADS, first_slot = wave * turns * 64;
-    uint32_t image[P > 0 ? P : 1];                      // of the weight, then the key
-    int32_t token[P > 0 ? P : 1];
-    if constexpr (P > 0) {
+// What a workgroup has of its slice: turn u of wave w is slots base + (w * EV_TURNS + u) * 64 ...
+struct EvictSlice {
+    int base, n, k, wave, lane;
+    uint32_t image[EV_TURNS];
+    int32_t token[EV_TURNS];
+    __device__ __forceinline__ int at(int u) const { return base + (wave * EV_TURNS + u) * 64; }
+    __device__ __forceinline__ unsigned long long live(int u) const { const int j = at(u); return j >= n ? 0ull : n - j >= 64 ? ~0ull : (1ull << (n - j)) - 1; }
+    __device__ __forceinline__ unsigned long long low(int u) const { const int j = at(u); return j >= k ? 0ull : k - j >= 64 ? ~0ull : (1ull << (k - j)) - 1; }
+    // (every slot, live or not: loads behind a branch would wait for each other)
+    __device__ __forceinline__ void load(const float* w, const int32_t* tok) {
 #pragma unroll
-        for (int u = 0; u < P; ++u) {
-            const int j = min(first_slot + u * 64 + lane, n - 1);
+        for (int u = 0; u < EV_TURNS; ++u) {
+            const int j = min(at(u) + lane, n - 1);
             image[u] = evict_image(w[j]);
             token[u] = tok[j];
         }
     }
-    // f(turn, image of the weight, token) for every turn
-    auto each = [&](auto&& f) {
-        if constexpr (P > 0) {
-#pragma unroll
-            for (int u = 0; u < P; ++u) f(u, image[u], token[u]);
-        } else {
-            for (int u0 = 0; u0 < turns; u0 += EV_BATCH) {
-                float wv[EV_BATCH];
-                int32_t tv[EV_BATCH];
-#pragma unroll
-                for (int u = 0; u < EV_BATCH; ++u) {
-                    const int j = min(first_slot + (u0 + u) * 64 + lane, n - 1);
-                    wv[u] = w[j];
-                    tv[u] = tok[j];
-                }
-#pragma unroll
-                for (int u = 0; u < EV_BATCH; ++u)
-                    if (u0 + u < turns) f(u0 + u, evict_image(wv[u]), tv[u]);
-            }
-        }
-    };
-    auto live_of = [&](int u) {                         // the turn's live slots
-        const int at = first_slot + u * 64;
-        return at >= n ? 0ull : n - at >= 64 ? ~0ull : (1ull << (n - at)) - 1;
-    };
-    // the last number, and the range of the images
-    int top = INT32_MIN;
-    uint32_t lo = ~0u, hi = 0;
-    each([&](int, uint32_t im, int32_t t) { top = max(top, t); lo = min(lo, im); hi = max(hi, im); });
+    __device__ __forceinline__ uint32_t key(int u, int first, long long newest) const { return token[u] < first || (long long)token[u] > newest ? EV_PROTECTED : image[u]; }
+};
+struct EvictLds {
+    int hist[EV_BINS];
+    int a[EV_WAVES], b[EV_WAVES], c[EV_WAVES];
+    uint32_t lo[EV_WAVES], hi[EV_WAVES];
+    int digit, above, equal;
+};
+// the search: keys lo + (bin << shift) ..., `need` of them still to be found from the top
+struct EvictSearch {
+    uint32_t lo, limit, span;
+    int shift, need, equal;
+    bool first, found;
+    __device__ __forceinline__ void start(uint32_t low, uint32_t high, int k) {
+        lo = low; need = k; equal = 0; limit = 0; span = 0; first = true; found = false;
+        shift = 0;
+        while (((high - low) >> shift) > EV_BINS - 2) ++shift;         // the last bin is the protected ones'
+    }
+    // the bin of a key, -1 for one that is out already
+    __device__ __forceinline__ int bin(uint32_t key) const {
+        if (first) return key == EV_PROTECTED ? EV_BINS - 1 : (int)((key - lo) >> shift);
+        return key != EV_PROTECTED && key >= lo && key - lo <= span ? (int)((key - lo) >> shift) : -1;
+    }
+};
+// largest number, smallest and largest image of the workgroup's lanes
+__device__ __forceinline__ void evict_extremes(int& top, uint32_t& lo, uint32_t& hi, int wave, int lane, EvictLds& lds) {
     top = ev_reduce(top, [](int x, int y) { return max(x, y); });
     lo = (uint32_t)ev_reduce((int)lo, [](int x, int y) { return (int)min((uint32_t)x, (uint32_t)y); });
     hi = (uint32_t)ev_reduce((int)hi, [](int x, int y) { return (int)max((uint32_t)x, (uint32_t)y); });
-    if (lane == 0) { wave_a[wave] = top; wave_lo[wave] = lo; wave_hi[wave] = hi; }
-    hist[tid] = 0;
-    hist[tid + EV_THREADS] = 0;
+    if (lane == 0) { lds.a[wave] = top; lds.lo[wave] = lo; lds.hi[wave] = hi; }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < EV_WAVES; ++i) { top = max(top, wave_a[i]); lo = min(lo, wave_lo[i]); hi = max(hi, wave_hi[i]); }
-    const long long newest = (long long)top - a.recent;
-    auto key_of = [&](uint32_t im, int32_t t) { return t < a.first || (long long)t > newest ? EV_PROTECTED : im; };
-
-    // the k-th largest key, and how many of the keys equal to it stay
-    uint32_t limit = 0;
-    int need = 0, equal = 0;
-    if (k > 0 && k < n) {
-        int shift = 0;
-        while (((hi - lo) >> shift) > EV_BINS - 2) ++shift;
-        need = k;
-        bool first = true;
-        uint32_t span = 0;                              // of the keys that are left, behind the first time
-        while (true) {
-            each([&](int u, uint32_t im, int32_t t) {
-                const uint32_t key = key_of(im, t), at = key - lo;
-                const int bin = first && key == EV_PROTECTED ? EV_BINS - 1 : (int)(at >> shift);
-                if (((live_of(u) >> lane) & 1) && (first || (key != EV_PROTECTED && key >= lo && at <= span))) atomicAdd(&hist[bin], 1);
-            });
-            __syncthreads();
-            // counts from the last bin down: a thread has two
-            const int h1 = hist[EV_BINS - 1 - 2 * tid], h0 = hist[EV_BINS - 2 - 2 * tid];
-            const int sum = wave_incl_scan(h1 + h0);
-            if (lane == 63) wave_a[wave] = sum;
-            __syncthreads();
-            hist[tid] = 0;
-            hist[tid + EV_THREADS] = 0;
-            int above = sum - h1 - h0;
+    for (int i = 0; i < EV_WAVES; ++i) { top = max(top, lds.a[i]); lo = min(lo, lds.lo[i]); hi = max(hi, lds.hi[i]); }
+}
+// One step of the search: counts h1, h0 of this thread's two bins, from the last one down.  A barrier in front of it separates it from the use of lds.a before.
+__device__ __forceinline__ void evict_step(EvictSearch& s, int h1, int h0, int tid, EvictLds& lds) {
+    const int wave = tid >> 6, sum = wave_incl_scan(h1 + h0);
+    if ((tid & 63) == 63) lds.a[wave] = sum;
+    __syncthreads();
+    int above = sum - h1 - h0;
 #pragma unroll
-            for (int i = 0; i < EV_WAVES; ++i) above += i < wave ? wave_a[i] : 0;
-            if (above < need && need <= above + h1) { s_digit = EV_BINS - 1 - 2 * tid; s_above = above; s_equal = h1; }
-            else if (above + h1 < need && need <= above + h1 + h0) { s_digit = EV_BINS - 2 - 2 * tid; s_above = above + h1; s_equal = h0; }
-            __syncthreads();
-            const int digit = s_digit;
-            need -= s_above;
-            equal = s_equal;
-            if (first && digit == EV_BINS - 1) { limit = EV_PROTECTED; break; }
-            lo += (uint32_t)digit << shift;
-            if (shift == 0) { limit = lo; break; }
-            span = (1u << shift) - 1;
-            shift = max(shift - 11, 0);
-            first = false;
-        }
-    } else {
-        limit = k > 0 ? 0u : EV_PROTECTED;              // all stay, or none
-        equal = k > 0 ? 0 : n + 1;
-    }
-    // The words, in ascending order.  Of the keys equal to the k-th the first `need` stay: where that is not all of them, those in front are counted.
+    for (int i = 0; i < EV_WAVES; ++i) above += i < wave ? lds.a[i] : 0;
+    if (above < s.need && s.need <= above + h1) { lds.digit = EV_BINS - 1 - 2 * tid; lds.above = above; lds.equal = h1; }
+    else if (above + h1 < s.need && s.need <= above + h1 + h0) { lds.digit = EV_BINS - 2 - 2 * tid; lds.above = above + h1; lds.equal = h0; }
+    __syncthreads();
+    const int digit = lds.digit;
+    s.need -= lds.above;
+    s.equal = lds.equal;
+    if (s.first && digit == EV_BINS - 1) { s.limit = EV_PROTECTED; s.found = true; return; }
+    s.lo += (uint32_t)digit << s.shift;
+    if (s.shift == 0) { s.limit = s.lo; s.found = true; return; }
+    s.span = (1u << s.shift) - 1;
+    s.shift = max(s.shift - 11, 0);
+    s.first = false;
+}
+// The slice's words.  tied: keys equal to the limit in front of the slice, of which the first `need` stay; nh, nm: holes and movers in front of it.
+__device__ __forceinline__ void evict_words(const EvictArgs& a, const EvictSlice& sl, int b, uint32_t limit, int need, int equal, long long newest, int tied, int nh, int nm, EvictLds& lds) {
+    const int wave = sl.wave, lane = sl.lane;
     const bool count_ties = need < equal;
-    int tied = 0;
     if (count_ties) {
-        each([&](int u, uint32_t im, int32_t t) { tied += __popcll(__builtin_amdgcn_ballot_w64(key_of(im, t) == limit) & live_of(u)); });
-        if (lane == 0) wave_b[wave] = tied;
-        __syncthreads();
-        tied = 0;
+        int mine = 0;
 #pragma unroll
-        for (int i = 0; i < EV_WAVES; ++i) tied += i < wave ? wave_b[i] : 0;
+        for (int u = 0; u < EV_TURNS; ++u) mine += __popcll(__builtin_amdgcn_ballot_w64(sl.key(u, a.first, newest) == limit) & sl.live(u));
         __syncthreads();
+        if (lane == 0) lds.a[wave] = mine;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < EV_WAVES; ++i) tied += i < wave ? lds.a[i] : 0;
     }
-    const size_t row = (size_t)b * a.words + wave * turns;
-    const int words = min((n + 63) / 64 - wave * turns, turns);        // of this wave
-    const bool at_end = P > 0 || turns <= 64;
-    unsigned long long my_word = 0;
-    int my_h = 0, my_m = 0, nh = 0, nm = 0;             // lane u % 64 keeps what belongs to turn u, 64 turns are stored together
-    each([&](int u, uint32_t im, int32_t t) {
-        const uint32_t key = key_of(im, t);
-        const unsigned long long live = live_of(u);
-        unsigned long long word = __builtin_amdgcn_ballot_w64(key >= limit) & live;
+    unsigned long long word[EV_TURNS], my_word = 0;
+    int h = 0, m = 0, my_h = 0, my_m = 0;
+#pragma unroll
+    for (int u = 0; u < EV_TURNS; ++u) {
+        const uint32_t key = sl.key(u, a.first, newest);
+        const unsigned long long live = sl.live(u), low = sl.low(u);
+        word[u] = __builtin_amdgcn_ballot_w64(key >= limit) & live;
         if (count_ties) {
             unsigned long long same = __builtin_amdgcn_ballot_w64(key == limit) & live;
             const int there = __popcll(same), allowed = min(max(need - tied, 0), there);
             tied += there;
-            word &= ~same;
+            word[u] &= ~same;
             for (int i = there; i > allowed; --i) same &= ~(1ull << (63 - __clzll((long long)same)));
-            word |= same;
+            word[u] |= same;
         }
-        const int at = first_slot + u * 64;
-        const unsigned long long low = at >= k ? 0ull : k - at >= 64 ? ~0ull : (1ull << (k - at)) - 1;
-        const bool mine = lane == (u & 63);
-        my_word = mine ? word : my_word;
-        my_h = mine ? nh : my_h;
-        my_m = mine ? nm : my_m;
-        nh += __popcll(low & ~word);
-        nm += __popcll(word & ~low);
-        if (!at_end && ((u & 63) == 63 || u == turns - 1)) {
-            const int to = (u & ~63) + lane;
-            if (to <= u && to < words) { a.stays[row + to] = my_word; a.holes[row + to] = my_h; a.movers[row + to] = my_m; }
-        }
-    });
-    if (lane == 0) { wave_b[wave] = nh; wave_c[wave] = nm; }
-    __syncthreads();
-    nh = nm = 0;
-#pragma unroll
-    for (int i = 0; i < EV_WAVES; ++i) { nh += i < wave ? wave_b[i] : 0; nm += i < wave ? wave_c[i] : 0; }
-    // with the counts of the waves in front
-    for (int at = lane; at < words; at += 64) {
-        if (at_end) a.stays[row + at] = my_word;
-        a.holes[row + at] = (at_end ? my_h : a.holes[row + at]) + nh;
-        a.movers[row + at] = (at_end ? my_m : a.movers[row + at]) + nm;
+        if (lane == u) { my_word = word[u]; my_h = h; my_m = m; }      // lane u keeps what belongs to turn u
+        h += __popcll(low & ~word[u]);
+        m += __popcll(word[u] & ~low);
     }
-    if (tid == 0) a.sizes[b] = make_int2(n, k);
+    if (lane == 0) { lds.b[wave] = h; lds.c[wave] = m; }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < EV_WAVES; ++i) { nh += i < wave ? lds.b[i] : 0; nm += i < wave ? lds.c[i] : 0; }
+    if (lane < EV_TURNS && sl.at(lane) < sl.n) {
+        const size_t to = (size_t)b * a.words + sl.at(lane) / 64;
+        a.stays[to] = my_word;
+        a.holes[to] = my_h + nh;
+        a.movers[to] = my_m + nm;
+    }
+}
+#endif
+
+// a sample of one slice: everything in one workgroup
+__global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ EvictLds lds;
+    const int tid = threadIdx.x, b = blockIdx.x;
+    EvictSlice sl;
+    sl.base = 0; sl.wave = __builtin_amdgcn_readfirstlane(tid >> 6); sl.lane = tid & 63;
+    sl.n = a.cache.length(b, a.max_len);
+    sl.k = min(max(a.keep[b], 0), sl.n);
+    if (tid == 0) a.sizes[b] = make_int2(sl.n, sl.k);
+    if (sl.n == 0) return;
+    sl.load(a.weight_in + (size_t)b * a.stride, a.token_in + (size_t)b * a.stride);
+    int top = sl.token[0];
+    uint32_t lo = sl.image[0], hi = sl.image[0];
+#pragma unroll
+    for (int u = 1; u < EV_TURNS; ++u) { top = max(top, sl.token[u]); lo = min(lo, sl.image[u]); hi = max(hi, sl.image[u]); }
+    lds.hist[tid] = 0;
+    lds.hist[tid + EV_THREADS] = 0;
+    evict_extremes(top, lo, hi, sl.wave, sl.lane, lds);
+    const long long newest = (long long)top - a.recent;
+    // all stay, or none, unless the k-th key says which
+    uint32_t limit = sl.k > 0 ? 0u : EV_PROTECTED;
+    int need = 0, equal = sl.k > 0 ? 0 : sl.n + 1;
+    if (sl.k > 0 && sl.k < sl.n) {
+        EvictSearch s;
+        s.start(lo, hi, sl.k);
+        while (!s.found) {
+#pragma unroll
+            for (int u = 0; u < EV_TURNS; ++u) {
+                const int bin = s.bin(sl.key(u, a.first, newest));
+                if (((sl.live(u) >> sl.lane) & 1) && bin >= 0) atomicAdd(&lds.hist[bin], 1);
+            }
+            __syncthreads();
+            const int h1 = lds.hist[EV_BINS - 1 - 2 * tid], h0 = lds.hist[EV_BINS - 2 - 2 * tid];
+            lds.hist[EV_BINS - 1 - 2 * tid] = 0;        // (its own two, for the next time)
+            lds.hist[EV_BINS - 2 - 2 * tid] = 0;
+            evict_step(s, h1, h0, tid, lds);
+        }
+        limit = s.limit; need = s.need; equal = s.equal;
+    }
+    evict_words(a, sl, b, limit, need, equal, newest, 0, 0, 0, lds);
+#endif
+}
+
+// Several slices.  STEP 0: the slice's extremes, and the sample's counts cleared.  1 .. EV_LEVELS: the bins of that level counted, behind the search through the levels before.
+// EV_LEVELS + 1: larger and equal keys of the slice.  EV_LEVELS + 2: its words.
+template <int STEP>
+__global__ __launch_bounds__(EV_THREADS) void evict_slices_kernel(EvictArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ EvictLds lds;
+    const int tid = threadIdx.x, slice = blockIdx.x, b = blockIdx.y;
+    EvictSlice sl;
+    sl.base = slice * EV_SLICE; sl.wave = __builtin_amdgcn_readfirstlane(tid >> 6); sl.lane = tid & 63;
+    sl.n = a.cache.length(b, a.max_len);
+    sl.k = min(max(a.keep[b], 0), sl.n);
+    int32_t* bins = a.bins + (size_t)b * EV_LEVELS * EV_BINS;
+    if (STEP == 0) {
+        for (int i = slice * EV_THREADS + tid; i < EV_LEVELS * EV_BINS; i += a.slices * EV_THREADS) bins[i] = 0;
+        if (slice == 0 && tid == 0) a.sizes[b] = make_int2(sl.n, sl.k);
+    }
+    const int slices = (sl.n + EV_SLICE - 1) / EV_SLICE;               // that the sample has
+    if (slice >= slices) return;
+    sl.load(a.weight_in + (size_t)b * a.stride, a.token_in + (size_t)b * a.stride);
+    int4* ranges = a.ranges + (size_t)b * a.slices;
+    int top;
+    uint32_t lo, hi;
+    if (STEP == 0) {
+        top = sl.token[0];
+        lo = hi = sl.image[0];
+#pragma unroll
+        for (int u = 1; u < EV_TURNS; ++u) { top = max(top, sl.token[u]); lo = min(lo, sl.image[u]); hi = max(hi, sl.image[u]); }
+    } else {
+        const int4 r = ranges[min(tid, slices - 1)];                   // (256 slices at most)
+        top = r.x; lo = (uint32_t)r.y; hi = (uint32_t)r.z;
+    }
+    evict_extremes(top, lo, hi, sl.wave, sl.lane, lds);
+    if (STEP == 0) {
+        if (tid == 0) ranges[slice] = make_int4(top, (int)lo, (int)hi, 0);
+        return;
+    }
+    const long long newest = (long long)top - a.recent;
+    uint32_t limit = sl.k > 0 ? 0u : EV_PROTECTED;
+    int need = 0, equal = sl.k > 0 ? 0 : sl.n + 1;
+    EvictSearch s;
+    s.start(lo, hi, sl.k);
+    s.found = !(sl.k > 0 && sl.k < sl.n);
+    if (!s.found) {
+        constexpr int LEVELS = STEP - 1 < EV_LEVELS ? STEP - 1 : EV_LEVELS;            // counted so far
+        int h[LEVELS > 0 ? LEVELS : 1][2];
+#pragma unroll
+        for (int l = 0; l < LEVELS; ++l) { h[l][0] = bins[l * EV_BINS + EV_BINS - 1 - 2 * tid]; h[l][1] = bins[l * EV_BINS + EV_BINS - 2 - 2 * tid]; }
+#pragma unroll
+        for (int l = 0; l < LEVELS; ++l)
+            if (!s.found) {
+                __syncthreads();
+                evict_step(s, h[l][0], h[l][1], tid, lds);
+            }
+        limit = s.limit; need = s.need; equal = s.equal;
+    }
+    if (STEP <= EV_LEVELS) {
+        if (s.found) return;
+        lds.hist[tid] = 0;
+        lds.hist[tid + EV_THREADS] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < EV_TURNS; ++u) {
+            const int bin = s.bin(sl.key(u, a.first, newest));
+            if (((sl.live(u) >> sl.lane) & 1) && bin >= 0) atomicAdd(&lds.hist[bin], 1);
+        }
+        __syncthreads();
+        for (int i = tid; i < EV_BINS; i += EV_THREADS)
+            if (lds.hist[i]) atomicAdd(&bins[(STEP - 1) * EV_BINS + i], lds.hist[i]);
+        return;
+    }
+    int4* counts = a.counts + (size_t)b * a.slices;
+    if (STEP == EV_LEVELS + 1) {
+        int more = 0, same = 0, more_high = 0, same_high = 0;
+#pragma unroll
+        for (int u = 0; u < EV_TURNS; ++u) {
+            const uint32_t key = sl.key(u, a.first, newest);
+            const unsigned long long live = sl.live(u), low = sl.low(u);
+            const unsigned long long m = __builtin_amdgcn_ballot_w64(key > limit) & live, t = __builtin_amdgcn_ballot_w64(key == limit) & live;
+            more += __popcll(m & low); more_high += __popcll(m & ~low);
+            same += __popcll(t & low); same_high += __popcll(t & ~low);
+        }
+        __syncthreads();
+        if (sl.lane == 0) { lds.a[sl.wave] = more; lds.b[sl.wave] = same; lds.c[sl.wave] = more_high; lds.lo[sl.wave] = (uint32_t)same_high; }
+        __syncthreads();
+        if (tid == 0) {
+            int4 c = make_int4(0, 0, 0, 0);
+            for (int i = 0; i < EV_WAVES; ++i) { c.x += lds.a[i]; c.y += lds.b[i]; c.z += lds.c[i]; c.w += (int)lds.lo[i]; }
+            counts[slice] = c;
+        }
+        return;
+    }
+    // Larger and equal keys in front of the slice; of the equal ones the first `need` stay, so that holes and movers follow from them.
+    const int4 c = tid < slice ? counts[tid] : make_int4(0, 0, 0, 0);
+    int more = c.x, same = c.y, more_high = c.z, same_high = c.w;
+    auto add = [](int x, int y) { return x + y; };
+    more = ev_reduce(more, add); same = ev_reduce(same, add); more_high = ev_reduce(more_high, add); same_high = ev_reduce(same_high, add);
+    __syncthreads();
+    if (sl.lane == 0) { lds.a[sl.wave] = more; lds.b[sl.wave] = same; lds.c[sl.wave] = more_high; lds.lo[sl.wave] = (uint32_t)same_high; }
+    __syncthreads();
+    more = same = more_high = same_high = 0;
+#pragma unroll
+    for (int i = 0; i < EV_WAVES; ++i) { more += lds.a[i]; same += lds.b[i]; more_high += lds.c[i]; same_high += (int)lds.lo[i]; }
+    const bool all = sl.k == sl.n, none = sl.k == 0;
+    const int before = min(sl.base, sl.k), kept = all ? before : none ? 0 : more + min(need, same);              // slots below k in front, those that stay
+    const int moved = all || none ? 0 : more_high + min(need, same + same_high) - min(need, same);
+    __syncthreads();
+    evict_words(a, sl, b, limit, need, equal, newest, same + same_high, before - kept, moved, lds);
 #endif
 }
 
@@ -240,7 +347,8 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
 constexpr int EV_AT_ONCE = 4;
 typedef uint32_t ev_u32x4 __attribute__((ext_vector_type(4)));
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int lanes) {
-    __shared__ int from_s[64], to_s[64], s_start;
+    __shared__ int from_s[64], to_s[64], found_w[64], found_m[64], s_found;
+    __shared__ unsigned long long found_bits[64];
     const int b = blockIdx.y, tid = threadIdx.x;
     const int2 size = a.sizes[b];
     const int n = size.x, k = size.y, word = blockIdx.x, slot0 = word * 64;
@@ -249,35 +357,34 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int lanes)
     const size_t row = (size_t)b * a.words, at = (size_t)b * a.stride;
     const unsigned long long low = k - slot0 >= 64 ? ~0ull : (1ull << (k - slot0)) - 1, stay = a.stays[row + word] & low, hole = low & ~stay;
     const int h0 = a.holes[row + word], count = __popcll(hole);
-    // the word that has mover h0: the last one with at most h0 movers in front (words without any in between have none to give)
+    // Words that have some of movers h0 .. h0 + count - 1 (each has at least one: 64 at most), a thread to a word from k on.  The last ones' movers end with the holes.
     const int w0 = k >> 6, w1 = (n - 1) >> 6;
-    if (count > 0) {
-        for (int w = w0 + tid; w <= w1; w += 256) {
-            const int mine = a.movers[row + w];
-            if (mine <= h0 && (w == w1 || a.movers[row + w + 1] > h0)) s_start = w;
+    if (tid == 0) s_found = 0;
+    __syncthreads();
+    for (int w = w0 + tid; w <= w1; w += 256) {
+        const unsigned long long low_w = k - w * 64 >= 64 ? ~0ull : k <= w * 64 ? 0ull : (1ull << (k - w * 64)) - 1;
+        const int m = a.movers[row + w];
+        const unsigned long long movers = a.stays[row + w] & ~low_w;
+        if (movers && m < h0 + count && m + __popcll(movers) > h0) {
+            const int i = atomicAdd(&s_found, 1);       // (in no order: every mover has its own place)
+            found_w[i] = w; found_m[i] = m; found_bits[i] = movers;
         }
     }
     if (tid < 64) {
         const int j = slot0 + tid;
-        const unsigned long long in_front = (1ull << tid) - 1;
         if ((stay >> tid) & 1) {
             a.weight_out[at + j] = a.weight_in[at + j];
             a.token_out[at + j] = a.token_in[at + j];
             if (a.src) a.src[at + j] = j;
         }
-        if ((hole >> tid) & 1) to_s[__popcll(hole & in_front)] = j;
+        if ((hole >> tid) & 1) to_s[__popcll(hole & ((1ull << tid) - 1))] = j;
     }
-    if (count == 0) return;
     __syncthreads();
-    if (tid < 64) {
-        const unsigned long long in_front = (1ull << tid) - 1;
-        for (int w = s_start, got = a.movers[row + w] - h0; got < count && w <= w1; ++w) {
-            const unsigned long long low_w = k - w * 64 >= 64 ? ~0ull : k <= w * 64 ? 0ull : (1ull << (k - w * 64)) - 1;
-            const unsigned long long movers = a.stays[row + w] & ~low_w;
-            const int rank = got + __popcll(movers & in_front);
-            if (((movers >> tid) & 1) && rank >= 0 && rank < count) from_s[rank] = w * 64 + tid;
-            got += __popcll(movers);
-        }
+    const int lane = tid & 63;
+    for (int i = tid >> 6; i < s_found; i += 4) {       // a wave to a word
+        const unsigned long long movers = found_bits[i];
+        const int rank = found_m[i] - h0 + __popcll(movers & ((1ull << lane) - 1));
+        if (((movers >> lane) & 1) && rank >= 0 && rank < count) from_s[rank] = found_w[i] * 64 + lane;
     }
     __syncthreads();
     if (tid < count) {
@@ -308,16 +415,21 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int lanes)
     }
 }
 
-struct EvictWs { size_t sizes, stays, holes, movers, bytes; int words; };
+struct EvictWs { size_t sizes, stays, holes, movers, ranges, counts, bins, bytes; int words, slices; };
 static EvictWs evict_ws(int B, int max_len) {
     EvictWs w;
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 256); return at; };
     w.words = (max_len + 63) / 64;
+    w.slices = (max_len + EV_SLICE - 1) / EV_SLICE;
+    const size_t more = w.slices > 1 ? (size_t)B : 0;
     w.sizes = take((size_t)B * 8);
     w.stays = take((size_t)B * w.words * 8);
     w.holes = take((size_t)B * w.words * 4);
     w.movers = take((size_t)B * w.words * 4);
+    w.ranges = take(more * w.slices * 16);
+    w.counts = take(more * w.slices * 16);
+    w.bins = take(more * EV_LEVELS * EV_BINS * 4);
     w.bytes = o;
     return w;
 }
@@ -356,13 +468,19 @@ extern "C" int d3tom_cache_evict(const d3tom_paged_cache* cache, int max_len, co
     a.stays = (unsigned long long*)((char*)ws + w.stays);
     a.holes = (int32_t*)((char*)ws + w.holes); a.movers = (int32_t*)((char*)ws + w.movers);
     a.words = w.words;
+    a.slices = w.slices;
+    a.ranges = (int4*)((char*)ws + w.ranges); a.counts = (int4*)((char*)ws + w.counts); a.bins = (int32_t*)((char*)ws + w.bins);
     a.k_pages = (char*)cache->k_pages; a.v_pages = (char*)cache->v_pages;
     a.row_bytes = cache->Hkv * cache->dh * elem_bytes(cache->dt);
-#define D3TOM_SELECT(P) D3TOM_LAUNCH(EVICT_SELECT, st, (evict_select_kernel<P><<<cache->B, EV_THREADS, 0, st>>>(a)))
-    if (max_len <= 4 * EV_THREADS) D3TOM_SELECT(4);
-    else if (max_len <= 16 * EV_THREADS) D3TOM_SELECT(16);
-    else D3TOM_SELECT(0);
-#undef D3TOM_SELECT
+    if (w.slices == 1) {
+        D3TOM_LAUNCH(EVICT_SELECT, st, (evict_select_kernel<<<cache->B, EV_THREADS, 0, st>>>(a)));
+    } else {
+        static_assert(EV_LEVELS == 3 && D3TOM_MAX_EVICT_LEN <= EV_THREADS * EV_SLICE, "the launches below; a thread for every slice");
+        const dim3 grid(w.slices, cache->B);
+#define D3TOM_STEP(N) D3TOM_LAUNCH(EVICT_SELECT, st, (evict_slices_kernel<N><<<grid, EV_THREADS, 0, st>>>(a)))
+        D3TOM_STEP(0); D3TOM_STEP(1); D3TOM_STEP(2); D3TOM_STEP(3); D3TOM_STEP(4); D3TOM_STEP(5);
+#undef D3TOM_STEP
+    }
     int lanes = 0;                                      // log2 of the lanes of a move: one for each 16 bytes, a wave at most
     while (lanes < 6 && (16 << lanes) < 2 * a.row_bytes) ++lanes;
     const dim3 grid(w.words, cache->B);

@@ -434,6 +434,9 @@ def test_cache_evict(B, dtype, Hkv, dh, page, lens, keep, first, recent, aliased
 def test_cache_evict_ties_go_to_the_lower_slot(B, levels, odd):
     # few different weights (zeros of both signs, negative and tiny ones among them)
     _evict_case(B, "bf16", 1, 8, 16, [3000, 64, 2049], [1700, 13, 2048], 3, 5, levels=levels, odd=odd)
+    # the same over several slices of 4096 slots, ties on both sides of their borders and of the new end
+    _evict_case(B, "bf16", 1, 8, 16, [9000, 4097, 12288, 1, 8192, 0], [4500, 4096, 8192, 1, 100, 0], 3, 5, levels=levels, odd=odd)
+    _evict_case(B, "bf16", 1, 8, 16, [9000, 8200, 4096], [8999, 4097, 4095], 0, 0, levels=levels, odd=odd, aliased=True)
 
 
 def test_cache_evict_protects_by_number(B):
@@ -451,19 +454,20 @@ def test_cache_evict_protects_by_number(B):
 
 def test_cache_evict_weights_of_any_bits(B):
     # NaN weights (outside the contract) still leave keep slots, every one a row of its own
-    rng = np.random.default_rng(9)
-    c = Cache(B, [3000], 1, 8, 16, "bf16", seed=0)
-    w = torch.from_numpy(rng.integers(-2 ** 31, 2 ** 31, (1, 3000)).astype(np.int32)).cuda()
-    w[0, ::7] = -1                                                # all bits
-    w[0, 1::7] = 0x7FFFFFFF
-    src, left, tok = torch.full((1, 3000), -3, dtype=torch.int32, device="cuda"), _i32([0]), _i32(rng.permutation(3000)[None])
-    for keep in (1, 200, 430, 1500, 2999):
-        B.d3tom_cache_evict(c.handle, 3000, _i32([keep]), 3, 11, w.view(torch.float32), tok, torch.zeros(1, 3000, device="cuda"), torch.zeros_like(tok), left,
-                            B.workspace(B.d3tom_cache_evict_workspace_bytes(c.handle, 3000)), src=src)
-        got = src[0, :keep].cpu().numpy()
-        assert int(left[0]) == keep and len(set(got.tolist())) == keep and got.min() >= 0 and got.max() < 3000
-        moved = got != np.arange(keep)
-        assert (got[moved] >= keep).all() and (np.diff(got[moved]) > 0).all()
+    for n in (3000, 9001):
+        rng = np.random.default_rng(9)
+        c = Cache(B, [n], 1, 8, 16, "bf16", seed=0)
+        w = torch.from_numpy(rng.integers(-2 ** 31, 2 ** 31, (1, n)).astype(np.int32)).cuda()
+        w[0, ::7] = -1                                            # all bits
+        w[0, 1::7] = 0x7FFFFFFF
+        src, left, tok = torch.full((1, n), -3, dtype=torch.int32, device="cuda"), _i32([0]), _i32(rng.permutation(n)[None])
+        for keep in (1, 200, 430, n // 2, n - 1):
+            B.d3tom_cache_evict(c.handle, n, _i32([keep]), 3, 11, w.view(torch.float32), tok, torch.zeros(1, n, device="cuda"), torch.zeros_like(tok), left,
+                                B.workspace(B.d3tom_cache_evict_workspace_bytes(c.handle, n)), src=src)
+            got = src[0, :keep].cpu().numpy()
+            assert int(left[0]) == keep and len(set(got.tolist())) == keep and got.min() >= 0 and got.max() < n
+            moved = got != np.arange(keep)
+            assert (got[moved] >= keep).all() and (np.diff(got[moved]) > 0).all()
 
 
 # ---- together ---------------------------------------------------------------------------------------------------------------------------
