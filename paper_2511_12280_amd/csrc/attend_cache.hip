@@ -29,15 +29,6 @@ struct AttendCacheArgs {
     int weight_stride;
 };
 
-// x / d of numbers below 2^24, `per` = 1 / d: the float quotient is less than one off.  (The integer division is 40 instructions, and a kernel has a handful of
-// them in front of its first load.)
-__device__ __forceinline__ int div_by(int x, int d, float per) {
-    int q = (int)((float)x * per);
-    q -= q * d > x ? 1 : 0;
-    q += (q + 1) * d <= x ? 1 : 0;
-    return q;
-}
-
 // A sample's rows: first one, how many.  Offsets that do not fit are cut to what there is.
 __device__ __forceinline__ int sample_rows(const AttendCacheArgs& a, int b, int& r0) {
     r0 = min(max(a.q_off[b], 0), a.rows);

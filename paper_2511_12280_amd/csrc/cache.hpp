@@ -20,6 +20,15 @@ struct CacheView {
     __device__ __forceinline__ int length(int b, int max_len) const { return min(max(len[b], 0), max_len); }
 };
 
+// x / d of numbers below 2^24, `per` = 1 / d: the float quotient is less than one off.  (The integer division is 40 instructions, and a kernel has a handful of
+// them in front of its first load.)
+__device__ __forceinline__ int div_by(int x, int d, float per) {
+    int q = (int)((float)x * per);
+    q -= q * d > x ? 1 : 0;
+    q += (q + 1) * d <= x ? 1 : 0;
+    return q;
+}
+
 inline CacheView cache_view(const d3tom_paged_cache& c) {
     CacheView v;
     v.table = c.page_table; v.len = c.kv_len;

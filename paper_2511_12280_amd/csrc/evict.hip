@@ -7,7 +7,7 @@
 // bit for every slot that stays, and for each word of 64 how many holes (slots below k that do not stay) and movers (slots from k on that do) lie in front
 // of it: there are as many of either.
 //
-// A sample of one slice of 4096 slots is a single workgroup's, its keys in registers.  Longer caches are cut into slices with a workgroup each, in a launch for every step:
+// A sample of up to 16384 slots is a single workgroup's, its keys in registers.  Longer caches are cut into slices with a workgroup each, in a launch for every step:
 // what a step needs of all slices is small and read by every workgroup.  (One workgroup for 65521 slots took 72 us at best: a compute unit waits 2 us for a batch of
 // 64 KB, four times eight batches.)
 //
@@ -17,7 +17,8 @@
 
 namespace d3tom {
 
-constexpr int EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64, EV_BINS = 2048, EV_TURNS = 4, EV_SLICE = EV_THREADS * EV_TURNS, EV_LEVELS = 3;
+constexpr int EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64, EV_BINS = 2048, EV_LEVELS = 3;
+constexpr int EV_TURNS = 4, EV_SLICE = EV_THREADS * EV_TURNS, EV_ALONE_TURNS = 16;        // of 64 slots, of a wave: in slices; of a workgroup alone, at most
 
 struct EvictArgs {
     CacheView cache;
@@ -39,6 +40,7 @@ struct EvictArgs {
     int slices;
     int4 *ranges, *counts;
     int32_t* bins;
+    struct EvictSearch* searches;               // [B, steps]: the search behind each level
     char *k_pages, *v_pages;
     int row_bytes;
 };
@@ -69,19 +71,35 @@ __device__ __forceinline__ int ev_reduce(int v, F&& f) {
 #endif
 }
 
+// the search: keys lo + (bin << shift) ..., `need` of them still to be found from the top
+struct EvictSearch {
+    uint32_t lo, limit, span;
+    int shift, need, equal;
+    int first, found;
+    __device__ __forceinline__ void start(uint32_t low, uint32_t high, int k) {
+        lo = low; need = k; equal = 0; limit = 0; span = 0; first = true; found = false;
+        shift = 0;
+        while (((high - low) >> shift) > EV_BINS - 2) ++shift;         // the last bin is the protected ones'
+    }
+    // the bin of a key, -1 for one that is out already
+    __device__ __forceinline__ int bin(uint32_t key) const {
+        if (first) return key == EV_PROTECTED ? EV_BINS - 1 : (int)((key - lo) >> shift);
+        return key != EV_PROTECTED && key >= lo && key - lo <= span ? (int)((key - lo) >> shift) : -1;
+    }
+};
 #if defined(__HIP_DEVICE_COMPILE__)
 // What a workgroup has of its slice: turn u of wave w is slots base + (w * EV_TURNS + u) * 64 ...
-struct EvictSlice {
+template <int TURNS> struct EvictSlice {
     int base, n, k, wave, lane;
-    uint32_t image[EV_TURNS];
-    int32_t token[EV_TURNS];
-    __device__ __forceinline__ int at(int u) const { return base + (wave * EV_TURNS + u) * 64; }
+    uint32_t image[TURNS];
+    int32_t token[TURNS];
+    __device__ __forceinline__ int at(int u) const { return base + (wave * TURNS + u) * 64; }
     __device__ __forceinline__ unsigned long long live(int u) const { const int j = at(u); return j >= n ? 0ull : n - j >= 64 ? ~0ull : (1ull << (n - j)) - 1; }
     __device__ __forceinline__ unsigned long long low(int u) const { const int j = at(u); return j >= k ? 0ull : k - j >= 64 ? ~0ull : (1ull << (k - j)) - 1; }
     // (every slot, live or not: loads behind a branch would wait for each other)
     __device__ __forceinline__ void load(const float* w, const int32_t* tok) {
 #pragma unroll
-        for (int u = 0; u < EV_TURNS; ++u) {
+        for (int u = 0; u < TURNS; ++u) {
             const int j = min(at(u) + lane, n - 1);
             image[u] = evict_image(w[j]);
             token[u] = tok[j];
@@ -94,22 +112,6 @@ struct EvictLds {
     int a[EV_WAVES], b[EV_WAVES], c[EV_WAVES];
     uint32_t lo[EV_WAVES], hi[EV_WAVES];
     int digit, above, equal;
-};
-// the search: keys lo + (bin << shift) ..., `need` of them still to be found from the top
-struct EvictSearch {
-    uint32_t lo, limit, span;
-    int shift, need, equal;
-    bool first, found;
-    __device__ __forceinline__ void start(uint32_t low, uint32_t high, int k) {
-        lo = low; need = k; equal = 0; limit = 0; span = 0; first = true; found = false;
-        shift = 0;
-        while (((high - low) >> shift) > EV_BINS - 2) ++shift;         // the last bin is the protected ones'
-    }
-    // the bin of a key, -1 for one that is out already
-    __device__ __forceinline__ int bin(uint32_t key) const {
-        if (first) return key == EV_PROTECTED ? EV_BINS - 1 : (int)((key - lo) >> shift);
-        return key != EV_PROTECTED && key >= lo && key - lo <= span ? (int)((key - lo) >> shift) : -1;
-    }
 };
 // largest number, smallest and largest image of the workgroup's lanes
 __device__ __forceinline__ void evict_extremes(int& top, uint32_t& lo, uint32_t& hi, int wave, int lane, EvictLds& lds) {
@@ -143,43 +145,44 @@ __device__ __forceinline__ void evict_step(EvictSearch& s, int h1, int h0, int t
     s.first = false;
 }
 // The slice's words.  tied: keys equal to the limit in front of the slice, of which the first `need` stay; nh, nm: holes and movers in front of it.
-__device__ __forceinline__ void evict_words(const EvictArgs& a, const EvictSlice& sl, int b, uint32_t limit, int need, int equal, long long newest, int tied, int nh, int nm, EvictLds& lds) {
+template <int TURNS>
+__device__ __forceinline__ void evict_words(const EvictArgs& a, const EvictSlice<TURNS>& sl, int b, uint32_t limit, int need, int equal, long long newest, int tied, int nh, int nm, EvictLds& lds) {
     const int wave = sl.wave, lane = sl.lane;
     const bool count_ties = need < equal;
     if (count_ties) {
         int mine = 0;
 #pragma unroll
-        for (int u = 0; u < EV_TURNS; ++u) mine += __popcll(__builtin_amdgcn_ballot_w64(sl.key(u, a.first, newest) == limit) & sl.live(u));
+        for (int u = 0; u < TURNS; ++u) mine += __popcll(__builtin_amdgcn_ballot_w64(sl.key(u, a.first, newest) == limit) & sl.live(u));
         __syncthreads();
         if (lane == 0) lds.a[wave] = mine;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < EV_WAVES; ++i) tied += i < wave ? lds.a[i] : 0;
     }
-    unsigned long long word[EV_TURNS], my_word = 0;
+    unsigned long long my_word = 0;
     int h = 0, m = 0, my_h = 0, my_m = 0;
 #pragma unroll
-    for (int u = 0; u < EV_TURNS; ++u) {
+    for (int u = 0; u < TURNS; ++u) {
         const uint32_t key = sl.key(u, a.first, newest);
         const unsigned long long live = sl.live(u), low = sl.low(u);
-        word[u] = __builtin_amdgcn_ballot_w64(key >= limit) & live;
+        unsigned long long word = __builtin_amdgcn_ballot_w64(key >= limit) & live;
         if (count_ties) {
             unsigned long long same = __builtin_amdgcn_ballot_w64(key == limit) & live;
             const int there = __popcll(same), allowed = min(max(need - tied, 0), there);
             tied += there;
-            word[u] &= ~same;
+            word &= ~same;
             for (int i = there; i > allowed; --i) same &= ~(1ull << (63 - __clzll((long long)same)));
-            word[u] |= same;
+            word |= same;
         }
-        if (lane == u) { my_word = word[u]; my_h = h; my_m = m; }      // lane u keeps what belongs to turn u
-        h += __popcll(low & ~word[u]);
-        m += __popcll(word[u] & ~low);
+        if (lane == u) { my_word = word; my_h = h; my_m = m; }      // lane u keeps what belongs to turn u
+        h += __popcll(low & ~word);
+        m += __popcll(word & ~low);
     }
     if (lane == 0) { lds.b[wave] = h; lds.c[wave] = m; }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < EV_WAVES; ++i) { nh += i < wave ? lds.b[i] : 0; nm += i < wave ? lds.c[i] : 0; }
-    if (lane < EV_TURNS && sl.at(lane) < sl.n) {
+    if (lane < TURNS && sl.at(lane) < sl.n) {
         const size_t to = (size_t)b * a.words + sl.at(lane) / 64;
         a.stays[to] = my_word;
         a.holes[to] = my_h + nh;
@@ -188,12 +191,13 @@ __device__ __forceinline__ void evict_words(const EvictArgs& a, const EvictSlice
 }
 #endif
 
-// a sample of one slice: everything in one workgroup
+// everything in one workgroup, 1024 TURNS slots at most
+template <int TURNS>
 __global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ EvictLds lds;
     const int tid = threadIdx.x, b = blockIdx.x;
-    EvictSlice sl;
+    EvictSlice<TURNS> sl;
     sl.base = 0; sl.wave = __builtin_amdgcn_readfirstlane(tid >> 6); sl.lane = tid & 63;
     sl.n = a.cache.length(b, a.max_len);
     sl.k = min(max(a.keep[b], 0), sl.n);
@@ -203,7 +207,7 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
     int top = sl.token[0];
     uint32_t lo = sl.image[0], hi = sl.image[0];
 #pragma unroll
-    for (int u = 1; u < EV_TURNS; ++u) { top = max(top, sl.token[u]); lo = min(lo, sl.image[u]); hi = max(hi, sl.image[u]); }
+    for (int u = 1; u < TURNS; ++u) { top = max(top, sl.token[u]); lo = min(lo, sl.image[u]); hi = max(hi, sl.image[u]); }
     lds.hist[tid] = 0;
     lds.hist[tid + EV_THREADS] = 0;
     evict_extremes(top, lo, hi, sl.wave, sl.lane, lds);
@@ -216,7 +220,7 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
         s.start(lo, hi, sl.k);
         while (!s.found) {
 #pragma unroll
-            for (int u = 0; u < EV_TURNS; ++u) {
+            for (int u = 0; u < TURNS; ++u) {
                 const int bin = s.bin(sl.key(u, a.first, newest));
                 if (((sl.live(u) >> sl.lane) & 1) && bin >= 0) atomicAdd(&lds.hist[bin], 1);
             }
@@ -239,7 +243,7 @@ __global__ __launch_bounds__(EV_THREADS) void evict_slices_kernel(EvictArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ EvictLds lds;
     const int tid = threadIdx.x, slice = blockIdx.x, b = blockIdx.y;
-    EvictSlice sl;
+    EvictSlice<EV_TURNS> sl;
     sl.base = slice * EV_SLICE; sl.wave = __builtin_amdgcn_readfirstlane(tid >> 6); sl.lane = tid & 63;
     sl.n = a.cache.length(b, a.max_len);
     sl.k = min(max(a.keep[b], 0), sl.n);
@@ -275,16 +279,20 @@ __global__ __launch_bounds__(EV_THREADS) void evict_slices_kernel(EvictArgs a) {
     s.start(lo, hi, sl.k);
     s.found = !(sl.k > 0 && sl.k < sl.n);
     if (!s.found) {
-        constexpr int LEVELS = STEP - 1 < EV_LEVELS ? STEP - 1 : EV_LEVELS;            // counted so far
-        int h[LEVELS > 0 ? LEVELS : 1][2];
-#pragma unroll
-        for (int l = 0; l < LEVELS; ++l) { h[l][0] = bins[l * EV_BINS + EV_BINS - 1 - 2 * tid]; h[l][1] = bins[l * EV_BINS + EV_BINS - 2 - 2 * tid]; }
-#pragma unroll
-        for (int l = 0; l < LEVELS; ++l)
+        // the search as the launch before left it, and through the level that it counted
+        constexpr int LEVEL = STEP - 2;
+        EvictSearch* saved = a.searches + (size_t)b * EV_LEVELS;
+        if (LEVEL >= 0 && LEVEL < EV_LEVELS) {
+            const int h1 = bins[LEVEL * EV_BINS + EV_BINS - 1 - 2 * tid], h0 = bins[LEVEL * EV_BINS + EV_BINS - 2 - 2 * tid];
+            if (LEVEL > 0) s = saved[LEVEL > 0 ? LEVEL - 1 : 0];
             if (!s.found) {
                 __syncthreads();
-                evict_step(s, h[l][0], h[l][1], tid, lds);
+                evict_step(s, h1, h0, tid, lds);
             }
+            if (slice == 0 && tid == 0) saved[LEVEL < EV_LEVELS ? LEVEL : 0] = s;
+        } else if (LEVEL >= EV_LEVELS) {
+            s = saved[EV_LEVELS - 1];
+        }
         limit = s.limit; need = s.need; equal = s.equal;
     }
     if (STEP <= EV_LEVELS) {
@@ -342,13 +350,14 @@ __global__ __launch_bounds__(EV_THREADS) void evict_slices_kernel(EvictArgs a) {
 #endif
 }
 
-// The word's moves: 2^lanes lanes have the 16-byte chunks of one (a row of k and the one of v behind it), EV_AT_ONCE of them to a lane at once.  And
+// The word's moves, as one sequence of 16-byte chunks (a row of k and the one of v behind it, move after move): EV_AT_ONCE of them to a thread at once.  And
 // what the word's slots keep of numbers.  len_out may be the cache's lengths: nothing reads them any more.
-constexpr int EV_AT_ONCE = 4;
+constexpr int EV_AT_ONCE = 8;
 typedef uint32_t ev_u32x4 __attribute__((ext_vector_type(4)));
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int lanes) {
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, float per_chunks) {
     __shared__ int from_s[64], to_s[64], found_w[64], found_m[64], s_found;
     __shared__ unsigned long long found_bits[64];
+    __shared__ size_t from_at[64], to_at[64];
     const int b = blockIdx.y, tid = threadIdx.x;
     const int2 size = a.sizes[b];
     const int n = size.x, k = size.y, word = blockIdx.x, slot0 = word * 64;
@@ -388,40 +397,44 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int lanes)
     }
     __syncthreads();
     if (tid < count) {
-        const int to = to_s[tid], from = from_s[tid];
+        const int to = to_s[tid], from = from_s[tid], pt = a.cache.page_of(b, to), pf = a.cache.page_of(b, from);
+        to_at[tid] = a.cache.writable(pt) ? a.cache.row((uint32_t)pt, to) * a.row_bytes : ~(size_t)0;
+        from_at[tid] = a.cache.row(a.cache.readable(pf), from) * a.row_bytes;
         a.weight_out[at + to] = a.weight_in[at + from];
         a.token_out[at + to] = a.token_in[at + from];
         if (a.src) a.src[at + to] = from;
     }
-    const int half = a.row_bytes / 16, chunks = 2 * half, step = 1 << lanes, c0 = tid & (step - 1);
-    for (int i = tid >> lanes; i < count; i += 256 >> lanes) {
-        const int to = to_s[i], from = from_s[i];
-        const int pt = a.cache.page_of(b, to), pf = a.cache.page_of(b, from);
-        if (!a.cache.writable(pt)) continue;
-        const size_t dst = a.cache.row((uint32_t)pt, to) * a.row_bytes, of = a.cache.row(a.cache.readable(pf), from) * a.row_bytes;
-        for (int c = c0; c < chunks; c += step * EV_AT_ONCE) {
+    __syncthreads();
+    const int half = a.row_bytes / 16, chunks = 2 * half;
+    // (64 moves of rows of 64 MB at most: groups of moves whose chunks are below 2^24)
+    const int group = max(1, min(count, (1 << 24) / chunks - 1));
+    for (int i0 = 0; i0 < count; i0 += group) {
+        const int total = min(group, count - i0) * chunks;
+        for (int x0 = tid; x0 < total; x0 += 256 * EV_AT_ONCE) {
             ev_u32x4 v[EV_AT_ONCE];
+            char* dst[EV_AT_ONCE];
 #pragma unroll
             for (int u = 0; u < EV_AT_ONCE; ++u) {
-                const int x = min(c + u * step, chunks - 1);
-                v[u] = *reinterpret_cast<const ev_u32x4*>((x < half ? a.k_pages : a.v_pages) + of + (size_t)(x < half ? x : x - half) * 16);
+                const int x = min(x0 + u * 256, total - 1), i = div_by(x, chunks, per_chunks), c = x - i * chunks;
+                char* pages = (c < half ? a.k_pages : a.v_pages) + (size_t)(c < half ? c : c - half) * 16;
+                const size_t to = to_at[i0 + i];
+                dst[u] = to == ~(size_t)0 || x0 + u * 256 >= total ? nullptr : pages + to;
+                v[u] = *reinterpret_cast<const ev_u32x4*>(pages + from_at[i0 + i]);
             }
 #pragma unroll
-            for (int u = 0; u < EV_AT_ONCE; ++u) {
-                const int x = c + u * step;
-                if (x < chunks) *reinterpret_cast<ev_u32x4*>((x < half ? a.k_pages : a.v_pages) + dst + (size_t)(x < half ? x : x - half) * 16) = v[u];
-            }
+            for (int u = 0; u < EV_AT_ONCE; ++u)
+                if (dst[u]) *reinterpret_cast<ev_u32x4*>(dst[u]) = v[u];
         }
     }
 }
 
-struct EvictWs { size_t sizes, stays, holes, movers, ranges, counts, bins, bytes; int words, slices; };
+struct EvictWs { size_t sizes, stays, holes, movers, ranges, counts, bins, searches, bytes; int words, slices; };
 static EvictWs evict_ws(int B, int max_len) {
     EvictWs w;
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 256); return at; };
     w.words = (max_len + 63) / 64;
-    w.slices = (max_len + EV_SLICE - 1) / EV_SLICE;
+    w.slices = max_len <= EV_ALONE_TURNS * EV_THREADS ? 1 : (max_len + EV_SLICE - 1) / EV_SLICE;
     const size_t more = w.slices > 1 ? (size_t)B : 0;
     w.sizes = take((size_t)B * 8);
     w.stays = take((size_t)B * w.words * 8);
@@ -430,6 +443,7 @@ static EvictWs evict_ws(int B, int max_len) {
     w.ranges = take(more * w.slices * 16);
     w.counts = take(more * w.slices * 16);
     w.bins = take(more * EV_LEVELS * EV_BINS * 4);
+    w.searches = take(more * EV_LEVELS * sizeof(EvictSearch));
     w.bytes = o;
     return w;
 }
@@ -470,10 +484,13 @@ extern "C" int d3tom_cache_evict(const d3tom_paged_cache* cache, int max_len, co
     a.words = w.words;
     a.slices = w.slices;
     a.ranges = (int4*)((char*)ws + w.ranges); a.counts = (int4*)((char*)ws + w.counts); a.bins = (int32_t*)((char*)ws + w.bins);
+    a.searches = (EvictSearch*)((char*)ws + w.searches);
     a.k_pages = (char*)cache->k_pages; a.v_pages = (char*)cache->v_pages;
     a.row_bytes = cache->Hkv * cache->dh * elem_bytes(cache->dt);
-    if (w.slices == 1) {
-        D3TOM_LAUNCH(EVICT_SELECT, st, (evict_select_kernel<<<cache->B, EV_THREADS, 0, st>>>(a)));
+    if (max_len <= EV_SLICE) {
+        D3TOM_LAUNCH(EVICT_SELECT, st, (evict_select_kernel<EV_TURNS><<<cache->B, EV_THREADS, 0, st>>>(a)));
+    } else if (w.slices == 1) {
+        D3TOM_LAUNCH(EVICT_SELECT, st, (evict_select_kernel<EV_ALONE_TURNS><<<cache->B, EV_THREADS, 0, st>>>(a)));
     } else {
         static_assert(EV_LEVELS == 3 && D3TOM_MAX_EVICT_LEN <= EV_THREADS * EV_SLICE, "the launches below; a thread for every slice");
         const dim3 grid(w.slices, cache->B);
@@ -481,9 +498,7 @@ extern "C" int d3tom_cache_evict(const d3tom_paged_cache* cache, int max_len, co
         D3TOM_STEP(0); D3TOM_STEP(1); D3TOM_STEP(2); D3TOM_STEP(3); D3TOM_STEP(4); D3TOM_STEP(5);
 #undef D3TOM_STEP
     }
-    int lanes = 0;                                      // log2 of the lanes of a move: one for each 16 bytes, a wave at most
-    while (lanes < 6 && (16 << lanes) < 2 * a.row_bytes) ++lanes;
     const dim3 grid(w.words, cache->B);
-    D3TOM_LAUNCH(EVICT_MOVE, st, (evict_move_kernel<<<grid, 256, 0, st>>>(a, lanes)));
+    D3TOM_LAUNCH(EVICT_MOVE, st, (evict_move_kernel<<<grid, 256, 0, st>>>(a, 8.0f / (float)a.row_bytes)));
     return D3TOM_OK;
 }
