@@ -352,9 +352,9 @@ __global__ __launch_bounds__(EV_THREADS) void evict_slices_kernel(EvictArgs a) {
 
 // The word's moves, as one sequence of 16-byte chunks (a row of k and the one of v behind it, move after move): EV_AT_ONCE of them to a thread at once.  And
 // what the word's slots keep of numbers.  len_out may be the cache's lengths: nothing reads them any more.
-constexpr int EV_AT_ONCE = 8;
+constexpr int EV_AT_ONCE = 4, EV_MOVE_THREADS = 512;
 typedef uint32_t ev_u32x4 __attribute__((ext_vector_type(4)));
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, float per_chunks) {
+__global__ __launch_bounds__(EV_MOVE_THREADS) void evict_move_kernel(EvictArgs a, float per_chunks) {
     __shared__ int from_s[64], to_s[64], found_w[64], found_m[64], s_found;
     __shared__ unsigned long long found_bits[64];
     __shared__ size_t from_at[64], to_at[64];
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, float per_
     const int w0 = k >> 6, w1 = (n - 1) >> 6;
     if (tid == 0) s_found = 0;
     __syncthreads();
-    for (int w = w0 + tid; w <= w1; w += 256) {
+    for (int w = w0 + tid; w <= w1; w += EV_MOVE_THREADS) {
         const unsigned long long low_w = k - w * 64 >= 64 ? ~0ull : k <= w * 64 ? 0ull : (1ull << (k - w * 64)) - 1;
         const int m = a.movers[row + w];
         const unsigned long long movers = a.stays[row + w] & ~low_w;
@@ -390,7 +390,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, float per_
     }
     __syncthreads();
     const int lane = tid & 63;
-    for (int i = tid >> 6; i < s_found; i += 4) {       // a wave to a word
+    for (int i = tid >> 6; i < s_found; i += EV_MOVE_THREADS / 64) {       // a wave to a word
         const unsigned long long movers = found_bits[i];
         const int rank = found_m[i] - h0 + __popcll(movers & ((1ull << lane) - 1));
         if (((movers >> lane) & 1) && rank >= 0 && rank < count) from_s[rank] = found_w[i] * 64 + lane;
@@ -410,15 +410,15 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, float per_
     const int group = max(1, min(count, (1 << 24) / chunks - 1));
     for (int i0 = 0; i0 < count; i0 += group) {
         const int total = min(group, count - i0) * chunks;
-        for (int x0 = tid; x0 < total; x0 += 256 * EV_AT_ONCE) {
+        for (int x0 = tid; x0 < total; x0 += EV_MOVE_THREADS * EV_AT_ONCE) {
             ev_u32x4 v[EV_AT_ONCE];
             char* dst[EV_AT_ONCE];
 #pragma unroll
             for (int u = 0; u < EV_AT_ONCE; ++u) {
-                const int x = min(x0 + u * 256, total - 1), i = div_by(x, chunks, per_chunks), c = x - i * chunks;
+                const int x = min(x0 + u * EV_MOVE_THREADS, total - 1), i = div_by(x, chunks, per_chunks), c = x - i * chunks;
                 char* pages = (c < half ? a.k_pages : a.v_pages) + (size_t)(c < half ? c : c - half) * 16;
                 const size_t to = to_at[i0 + i];
-                dst[u] = to == ~(size_t)0 || x0 + u * 256 >= total ? nullptr : pages + to;
+                dst[u] = to == ~(size_t)0 || x0 + u * EV_MOVE_THREADS >= total ? nullptr : pages + to;
                 v[u] = *reinterpret_cast<const ev_u32x4*>(pages + from_at[i0 + i]);
             }
 #pragma unroll
@@ -499,6 +499,6 @@ extern "C" int d3tom_cache_evict(const d3tom_paged_cache* cache, int max_len, co
 #undef D3TOM_STEP
     }
     const dim3 grid(w.words, cache->B);
-    D3TOM_LAUNCH(EVICT_MOVE, st, (evict_move_kernel<<<grid, 256, 0, st>>>(a, 8.0f / (float)a.row_bytes)));
+    D3TOM_LAUNCH(EVICT_MOVE, st, (evict_move_kernel<<<grid, EV_MOVE_THREADS, 0, st>>>(a, 8.0f / (float)a.row_bytes)));
     return D3TOM_OK;
 }
