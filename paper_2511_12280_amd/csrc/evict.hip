@@ -78,8 +78,8 @@ struct EvictSearch {
     int first, found;
     __device__ __forceinline__ void start(uint32_t low, uint32_t high, int k) {
         lo = low; need = k; equal = 0; limit = 0; span = 0; first = true; found = false;
-        shift = 0;
-        while (((high - low) >> shift) > EV_BINS - 2) ++shift;         // the last bin is the protected ones'
+        shift = high > low ? max(21 - __clz((int)(high - low)), 0) : 0;
+        if (((high - low) >> shift) > EV_BINS - 2) ++shift;            // the last bin is the protected ones'
     }
     // the bin of a key, -1 for one that is out already
     __device__ __forceinline__ int bin(uint32_t key) const {
