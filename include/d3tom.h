@@ -498,7 +498,8 @@ typedef struct {
  *   q, k          [rows, H, dh], [rows, Hkv, dh] dt, rows q_stride / k_stride ELEMENTS apart (a multiple of 16 bytes; columns of a stacked
  *                 projection); one of the two may be NULL
  *   q_out, k_out  [rows, H, dh], [rows, Hkv, dh] dt contiguous; may be q / k themselves where those are contiguous
- *   dh            a multiple of 16 (bf16) or 8 (f32), at most 256 */
+ *   dh            a multiple of 16 (bf16) or 8 (f32), at most 256
+ * More than 16 million rows return D3TOM_ERR_UNSUPPORTED. */
 int d3tom_rope_axes(const void* q, int64_t q_stride, const void* k, int64_t k_stride, int dt, int rows, int H, int Hkv, int dh,
                     const d3tom_axes* axes /* host */, void* q_out, void* k_out, void* stream);
 
@@ -511,7 +512,7 @@ int d3tom_rope_axes(const void* q, int64_t q_stride, const void* k, int64_t k_st
  *   tokens       int32[rows] or NULL; with slot_token int32[B, slot_stride]: the slots' entries become the rows' (a token's number in
  *                its sample, which d3tom_cache_evict reads)
  *   slot_weight  float[B, slot_stride] or NULL: the slots' entries become 0
- * With axes dh is a multiple of 16 (bf16) or 8 (f32). */
+ * With axes dh is a multiple of 16 (bf16) or 8 (f32).  samples * max_new above 16 million returns D3TOM_ERR_UNSUPPORTED. */
 int d3tom_cache_append(const d3tom_paged_cache* cache /* host */, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                        const int32_t* new_off, int rows, int max_new, const d3tom_axes* axes /* host */,
                        const void* q, int64_t q_stride, int H, void* q_out,

@@ -1198,8 +1198,7 @@ extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_p
     if (!q_off || !ws || !(scale > 0.f) || !(scale < 3.0e38f)) return D3TOM_ERR_INVALID_ARG;
     if ((weight_in && !weight_out) || (weight_out && weight_stride < max_len)) return D3TOM_ERR_INVALID_ARG;
     const AttendCachePlan p = attend_cache_plan(*cache, rows, max_q, max_len, H, weight_out != nullptr);
-    const double most = 16000000.0;             // workgroups of 256 threads in a launch
-    if ((double)cache->B * max_q * H * p.S > most || (double)max_q * H > most) return D3TOM_ERR_UNSUPPORTED;
+    if ((double)cache->B * max_q * H * p.S > CACHE_MOST_GROUPS || (double)max_q * H > CACHE_MOST_GROUPS) return D3TOM_ERR_UNSUPPORTED;
     if (ws_bytes < attend_cache_ws_bytes(*cache, rows, max_q, max_len, H, weight_out != nullptr) || (((uintptr_t)ws) & 255u)) return D3TOM_ERR_WORKSPACE_TOO_SMALL;
     AttendCacheArgs a{};
     a.cache = cache_view(*cache);

@@ -50,6 +50,9 @@ inline int cache_check(const d3tom_paged_cache* c) {
     return D3TOM_OK;
 }
 
+// Workgroups of a launch: a dimension of a grid has fewer than 2^32 threads, and a workgroup 256 of them.
+constexpr double CACHE_MOST_GROUPS = 16000000.0;
+
 // rows of heads * dh elements, `stride` elements apart
 inline int rows_check(const void* p, int64_t stride, int heads, int dh, int dt) {
     if (!p || !aligned16(p) || heads < 1) return D3TOM_ERR_INVALID_ARG;

@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RowJob job, AxesArgs ax)
         const int b = blockIdx.y;
         int r0 = job.new_off[b], r1 = job.new_off[b + 1], n = job.cache.len[b];
         r0 = max(r0, 0);
-        r1 = min(r1, job.rows);
+        r1 = min(max(r1, 0), job.rows);
         if ((int)blockIdx.x >= r1 - r0) return;
         row += r0;
         const int slot = n - (r1 - r0) + (int)blockIdx.x;
@@ -161,7 +161,7 @@ extern "C" int d3tom_rope_axes(const void* q, int64_t q_stride, const void* k, i
     if (rc != D3TOM_OK) return rc;
     if (q && ((rc = rows_check(q, q_stride, H, dh, dt)) != D3TOM_OK || (rc = rows_check(q_out, (int64_t)H * dh, H, dh, dt)) != D3TOM_OK)) return rc;
     if (k && ((rc = rows_check(k, k_stride, Hkv, dh, dt)) != D3TOM_OK || (rc = rows_check(k_out, (int64_t)Hkv * dh, Hkv, dh, dt)) != D3TOM_OK)) return rc;
-    if (H > 65535 || Hkv > 65535) return D3TOM_ERR_UNSUPPORTED;
+    if ((q && H > 65535) || (k && Hkv > 65535) || rows > CACHE_MOST_GROUPS) return D3TOM_ERR_UNSUPPORTED;
     job.q = q; job.k = k; job.q_stride = q_stride; job.k_stride = k_stride;
     job.H = H; job.Hkv = Hkv; job.dh = dh; job.q_out = q_out; job.k_out = k_out; job.rows = rows;
     if (dt == D3TOM_BF16) D3TOM_LAUNCH(ROPE, st, (rope_rows_kernel<uint16_t, true, false><<<rows, 256, 0, st>>>(job, ax)));
@@ -183,7 +183,7 @@ extern "C" int d3tom_cache_append(const d3tom_paged_cache* cache, const void* k,
     AxesArgs ax{};
     if (axes && (rc = axes_check(axes, dh, dt, &ax)) != D3TOM_OK) return rc;
     if (q && ((rc = rows_check(q, q_stride, H, dh, dt)) != D3TOM_OK || (rc = rows_check(q_out, (int64_t)H * dh, H, dh, dt)) != D3TOM_OK)) return rc;
-    if (q && H > 65535) return D3TOM_ERR_UNSUPPORTED;
+    if ((q && H > 65535) || (double)max_new * cache->B > CACHE_MOST_GROUPS) return D3TOM_ERR_UNSUPPORTED;
     RowJob job{};
     job.q = q; job.k = k; job.v = v; job.q_stride = q_stride; job.k_stride = k_stride; job.v_stride = v_stride;
     job.H = H; job.Hkv = cache->Hkv; job.dh = dh; job.q_out = q_out;

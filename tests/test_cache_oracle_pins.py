@@ -132,7 +132,8 @@ def test_rope_axes_refuses(B):
                dict(rows=0), dict(rows=-1), dict(H=0), dict(Hkv=0), dict(dt=2), dict(dh=0)):
         assert _rope(lib, good, **kw) == INVALID, kw
     assert _rope(lib, None) == INVALID
-    for kw in (dict(dh=72, qs=1024, ks=1024), dict(dh=264, qs=2048, ks=2048), dict(dh=260, dt=0, qs=2048, ks=2048)):
+    for kw in (dict(dh=72, qs=1024, ks=1024), dict(dh=264, qs=2048, ks=2048), dict(dh=260, dt=0, qs=2048, ks=2048), dict(rows=16000001), dict(rows=2 ** 31 - 1),
+               dict(H=65536, qs=1 << 22), dict(Hkv=65536, ks=1 << 22)):
         assert _rope(lib, good, **kw) == UNSUPPORTED, kw
 
 
@@ -153,6 +154,8 @@ def test_cache_append_refuses(B):
         assert _append(lib, B, **kw) == INVALID, kw
     assert lib.d3tom_cache_append(None, P, i64(128), P, i64(128), P, i32(5), i32(3), None, None, i64(0), i32(4), None, None, None, None, i32(0), None) == INVALID
     assert _append(lib, B, cache=_cache(B, dh=8), ks=16, vs=16, axes=_axes(B, pairs=(1, 1, 1, 0))) == UNSUPPORTED
+    for kw in (dict(rows=16000001, most=16000001), dict(cache=_cache(B, B=65535), rows=4000, most=245), dict(axes=_axes(B), q=P, qo=P, H=65536, qs=1 << 22)):
+        assert _append(lib, B, **kw) == UNSUPPORTED, kw
 
 
 def _attend(lib, B, cache=None, q=P, qs=256, off=P, rows=5, most=3, max_len=320, H=4, scale=0.125, causal=0, o=P, lse=None, wi=None, wo=None, stride=0, ws=P,

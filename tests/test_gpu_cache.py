@@ -383,13 +383,15 @@ def test_attend_and_append_in_a_cache_above_four_gigabytes(B):
 
 
 # ---- eviction ----------------------------------------------------------------------------------------------------------------------
-def _evict_case(B, dtype, Hkv, dh, page, lens, keep, first, recent, seed=0, levels=0, aliased=False, odd=0):
+def _evict_case(B, dtype, Hkv, dh, page, lens, keep, first, recent, seed=0, levels=0, aliased=False, odd=0, weights=None):
     c = Cache(B, lens, Hkv, dh, page, dtype, seed=[seed, len(lens), page])
     rng = np.random.default_rng([seed, 4])
     W = max(max(lens), 1) + 3
     w = np.exp(2 * rng.standard_normal((len(lens), W)) - 4).astype(np.float32)
     if levels:
         w = rng.integers(0, levels, w.shape).astype(np.float32) * (-1.0 if odd else 1.0) * np.float32(1e-30 if odd == 2 else 1.0)
+    if weights is not None:
+        w[:, :weights.shape[1]] = weights
     tok = np.stack([rng.permutation(W) for _ in lens]).astype(np.int32)
     dw, dt = _dev(w, "f32"), _i32(tok)
     w_out, t_out = (dw, dt) if aliased else (torch.full(w.shape, -3.0, device="cuda"), torch.full(w.shape, -3, dtype=torch.int32, device="cuda"))
@@ -437,6 +439,20 @@ def test_cache_evict_ties_go_to_the_lower_slot(B, levels, odd):
     # the same over several slices of 4096 slots, ties on both sides of their borders and of the new end
     _evict_case(B, "bf16", 1, 8, 16, [9000, 4097, 12288, 1, 8192, 0], [4500, 4096, 8192, 1, 100, 0], 3, 5, levels=levels, odd=odd)
     _evict_case(B, "bf16", 1, 8, 16, [9000, 8200, 4096], [8999, 4097, 4095], 0, 0, levels=levels, odd=odd, aliased=True)
+
+
+@pytest.mark.parametrize("n", [4000, 5000])
+@pytest.mark.parametrize("cluster,ties", [(2, 1), (63, 1), (64, 1), (65, 1), (64, 3), (66, 2), (64, 64)])
+def test_cache_evict_weights_close_together(B, n, cluster, ties):
+    # `cluster` weights, `ties` of each, whose bits differ in the last places only, among others far below and above: all of them share a bin of the first count
+    rng = np.random.default_rng([n, cluster, ties])
+    w = np.where(rng.random(n) < 0.4, 4 + 4 * rng.random(n), 0.25 * rng.random(n)).astype(np.float32)
+    w[7] = 0
+    at = 8 + rng.permutation(n - 8)[:cluster]
+    w[at] = (np.float32(1).view(np.int32) + np.arange(cluster, dtype=np.int32) // ties).view(np.float32)
+    above = int((w > 3).sum())
+    for keep in {above + 1, above + 2, above + cluster // 2, above + cluster - 1, above + cluster}:
+        _evict_case(B, "bf16", 1, 8, 16, [n], [keep], 0, 0, weights=w[None])
 
 
 def test_cache_evict_protects_by_number(B):
