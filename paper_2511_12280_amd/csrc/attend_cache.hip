@@ -155,7 +155,8 @@ __global__ __launch_bounds__(256) void attend_cache_generic_kernel(AttendCacheAr
 //
 // Bound by memory: a key's row is read for 16 columns at most.  What keeps it busy is bytes in flight, so every wave is on its own, with a ring of two stages (K and V of
 // 8 KB each) that direct loads fill: while one stage is used the other and the next are on their way, and no wave waits for another one before
-// the end, when the four waves of a workgroup join what they have through LDS.
+// the end, when the four waves of a workgroup join what they have through LDS.  One row each of two samples of 131071 slots, 32 heads over 8 of 128, bf16:
+// 186 us, 5.8 TB/s.  One row of 3709 slots, 32 key heads: 13 us, 4.7 TB/s.
 template <typename T, int DH> struct AcTile {
     static constexpr int ROWB = DH * (int)sizeof(T), NCHK = ROWB / 16;      // bytes and 16-byte chunks of a row of a head
     static constexpr int TILE = 8192, KEYS = TILE / ROWB, KB = KEYS / 16;   // of K or V: keys, blocks of 16
@@ -843,7 +844,9 @@ __device__ __forceinline__ void rows_lse2(const AttendCacheArgs& a, int r0, int 
 // 4 bytes a logit there and back).  A workgroup has a tile of a sample's slots and goes over all heads and rows, wave w over key heads w, w + 8, ...
 // (or parts of a head's rows where there are fewer), each wave on its own.  The keys of a head come through LDS into its registers, then the queries, 16 rows at a time with
 // their lse, through a ring in the same place.  (Loaded as fragments, 64 bytes of a row at a time, the keys took 6700 clocks and every block of queries 2000.)
-// In the end bound by vector instructions: an fma, an exp2 and an addition a logit.  (The rows' lse come from the joining launch in front: formed by every
+// In the end bound by vector instructions: an fma, an exp2 and an addition a logit.  Four samples of 1951 .. 3773 slots and 32 rows, 32 heads over 8 of 128: 15.8 us; of a
+// workgroup's 32000 clocks the keys' way into LDS takes 9500 (23 MB), the first queries 3000, the blocks of rows 13000; the first wave
+// then waits up to 6000 for the others and the sums.  (The rows' lse come from the joining launch in front: formed by every
 // workgroup for itself in one launch with the joining, four samples of 128 rows to a key head took 27 us instead of 21.)
 constexpr int CW_WAVES = 8;
 template <typename T, int DH> struct CwTile {

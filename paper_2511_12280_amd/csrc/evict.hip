@@ -12,7 +12,9 @@
 // 64 KB, four times eight batches.)
 //
 // The last launch has a workgroup for every word below k: it pairs the word's holes with the movers of the same numbers and moves their rows.
-// Every mover lies at k or above and every hole below it, so that the moves need no order among themselves.  Bound by memory.
+// Every mover lies at k or above and every hole below it, so that the moves need no order among themselves.  Bound by memory where rows are many:
+// 65521 slots halved, rows of 2 KB: the moves 34 us of 63 (3.9 TB/s there and back), the selection's six launches the rest; 16 samples of 900 .. 2688 slots cut to nine
+// tenths: selection 9.7 us (a workgroup to a sample, step behind step), moves 8.0.
 #include "cache.hpp"
 
 namespace d3tom {
@@ -234,7 +236,7 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
             if (TURNS > EV_TURNS && !s.found && s.equal <= 64) {
                 // The bin's keys, in no order, one to a lane of every wave: bit by bit, those with the bit are in front.  Instead of further passes over all slots:
                 // a call for one sample of 4200, 8192 and 16384 slots 22.9, 27.7 and 24.6 us with the passes, 21.1, 26.2 and 23.2 with this.  With 4 turns a pass is
-                // short and this the longer way (selection in 16 samples of 2688 slots: 9.7 us with the passes, 10.2 with this).
+                // short and this the longer way (selection in 16 samples of 900 .. 2688 slots: 9.7 us with the passes, 10.2 with this).
                 if (tid == 0) lds.listed = 0;
                 __syncthreads();
 #pragma unroll
