@@ -486,10 +486,13 @@ def d3tom_stack_step_batch(x: torch.Tensor, N: Sequence[int], H: int, F: int, bl
 # ---- the key/value cache in pages -----------------------------------------------------------------------------
 def _on(stream):
     """A call's stream and its device; tensors of another device are refused (work of one device on another's stream would not be
-    ordered with anything).  Sizes, types and devices of the tensors are checked where they are read, csrc/native.cpp: ValueError."""
-    if stream is not None:
-        return stream.cuda_stream, stream.device_index
+    ordered with anything), and so is a stream of another device than the current one, on which a launch would go.  Sizes, types and devices
+    of the tensors are checked where they are read, csrc/native.cpp: ValueError."""
     device = torch._C._cuda_getDevice()
+    if stream is not None:
+        if stream.device_index != device:
+            raise ValueError("the stream is of another device than the current one")
+        return stream.cuda_stream, device
     return torch._C._cuda_getCurrentRawStream(device), device
 
 

@@ -220,6 +220,15 @@ def test_cache_evict_refuses(B):
     assert _evict(lib, B, cache=large, max_len=(1 << 20) + 1, stride=1 << 21) == UNSUPPORTED
 
 
+def test_binding_refuses_a_stream_of_another_device(B, monkeypatch):
+    import torch
+    from types import SimpleNamespace
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    assert B._on(SimpleNamespace(cuda_stream=17, device_index=0)) == (17, 0)
+    with pytest.raises(ValueError, match="another device"):
+        B._on(SimpleNamespace(cuda_stream=17, device_index=1))
+
+
 def test_binding_refuses_what_it_cannot_pass_on(B):
     import torch
     t = torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16)

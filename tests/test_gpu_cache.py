@@ -192,10 +192,10 @@ def test_cache_append_skips_what_has_no_place(B):
 
 
 # ---- attention ------------------------------------------------------------------------------------------------------------------
-def _attend_case(B, dtype, H, Hkv, dh, page, lens, new, causal, weighed, seed=0, apart=False, std=1.0, behind=-1, scale=None, check=True):
+def _attend_case(B, dtype, H, Hkv, dh, page, lens, new, causal, weighed, seed=0, apart=False, std=1.0, behind=-1, scale=None, check=True, pad=0, more_q=0, more_len=0):
     c = Cache(B, lens, Hkv, dh, page, dtype, seed=[seed, dh, page, len(lens)], behind=behind, std=std)
     rng = np.random.default_rng([seed, 9])
-    rows, off = sum(new), _off(new)
+    rows, off = sum(new) + pad, _off(new)
     q = _round(rng.standard_normal((rows, H, dh)), dtype)
     scale = 1.0 / np.sqrt(dh) if scale is None else scale
     dq = _rows(q, dtype, apart)
@@ -204,7 +204,10 @@ def _attend_case(B, dtype, H, Hkv, dh, page, lens, new, causal, weighed, seed=0,
     W = max(lens) + 5
     w_in = rng.random((len(lens), W)).astype(np.float32) if weighed else None
     w_out = torch.full((len(lens), W), -3.0, device="cuda") if weighed else None
-    longest, most = max(max(lens), 1), max(new)
+    longest, most = max(max(lens), 1) + more_len, max(new) + more_q
+    W += more_len
+    if weighed and more_len:
+        w_in, w_out = np.pad(w_in, ((0, 0), (0, more_len))), torch.full((len(lens), W), -3.0, device="cuda")
     ws = torch.full((B.d3tom_attend_cache_workspace_bytes(c.handle, rows, most, longest, H, weighed),), 0xFF, dtype=torch.uint8, device="cuda")
     B.d3tom_attend_cache(dq, c.handle, _i32(off), most, longest, scale, causal, o, ws, lse=lse, weight_in=_dev(w_in, "f32") if weighed else None, weight_out=w_out)
     if check:
@@ -212,6 +215,7 @@ def _attend_case(B, dtype, H, Hkv, dh, page, lens, new, causal, weighed, seed=0,
             r = slice(off[b], off[b + 1])
             _check_attend(_host(o[r]), _host(lse[r]), _host(w_out[b]) if weighed else None, q[r], c.k[b], c.v[b], float(np.float32(scale)), causal, dtype,
                           w_in[b] if weighed else None)
+    assert (o[off[-1]:] == 7).all() and (lse[off[-1]:] == 7).all()
     return c, dq, o, lse, w_out, ws
 
 
@@ -259,6 +263,26 @@ ATTEND = [
 @pytest.mark.parametrize("weighed", [False, True])
 def test_attend_cache(B, dtype, H, Hkv, dh, page, lens, new, causal, weighed):
     _attend_case(B, dtype, H, Hkv, dh, page, lens, new, causal, weighed, apart=weighed, behind=-1 if weighed else 10 ** 8)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh,lens,new", [
+    ("bf16", 8, 2, 128, [100, 333, 50], [1, 0, 1]), ("bf16", 8, 2, 64, [100, 333, 50], [33, 0, 7]), ("bf16", 4, 2, 80, [100, 333], [0, 3]), ("f32", 8, 2, 64, [70, 300], [0, 40])])
+def test_attend_cache_samples_without_rows(B, dtype, H, Hkv, dh, lens, new):
+    # their slots' entries are what they were
+    _attend_case(B, dtype, H, Hkv, dh, 16, lens, new, False, True)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh,new,causal", [("bf16", 20, 10, 128, 40, False), ("bf16", 9, 9, 64, 35, True), ("f32", 17, 17, 64, 20, False), ("f32", 24, 12, 128, 11, True)])
+def test_attend_cache_weighs_more_key_heads_than_waves(B, dtype, H, Hkv, dh, new, causal):
+    _attend_case(B, dtype, H, Hkv, dh, 32, [270, 99], [new, 5], causal, True)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh,new,more_q", [("bf16", 8, 2, 128, [1, 1], 0), ("bf16", 8, 2, 128, [3, 1], 3), ("bf16", 8, 2, 64, [20, 2], 12), ("bf16", 8, 2, 128, [1, 2], 10),
+                                                       ("f32", 4, 4, 64, [5, 1], 4), ("bf16", 4, 2, 96, [2, 1], 6)])
+@pytest.mark.parametrize("weighed", [False, True])
+def test_attend_cache_padded_rows_and_generous_maxima(B, dtype, H, Hkv, dh, new, more_q, weighed):
+    # rows behind the last sample's are left as they were; max_q and max_len may exceed what there is
+    _attend_case(B, dtype, H, Hkv, dh, 16, [200, 131], new, True, weighed, pad=13, more_q=more_q, more_len=17)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -602,6 +626,105 @@ def test_captured_steps_on_another_stream(B):
         for b, n in enumerate([499, 300]):
             assert torch.equal(M.weight[b, :n], E.weight[b, :n]) and torch.equal(M.token[b, :n], E.token[b, :n])
     assert torch.isfinite(out_m["o"]).all()
+
+
+def test_two_graphs_share_a_workspace(B):
+    # a step for few rows with its logits kept and one for many rows, captured one by one on the same workspace and replayed in turn: nothing is carried from one to the other
+    nB, H, Hkv, dh, lens = 2, 8, 2, 128, [700, 300]
+    c = Cache(B, lens, Hkv, dh, 16, "bf16", seed=7)
+    calls = []
+    for m in (1, 24):
+        q = torch.randn(nB * m, H, dh, device="cuda").bfloat16()
+        calls.append(dict(q=q, off=_i32([0, m, 2 * m]), m=m, o=torch.zeros_like(q), w=torch.zeros(nB, 700, device="cuda")))
+    ws = B.workspace(max(B.d3tom_attend_cache_workspace_bytes(c.handle, 2 * x["m"], x["m"], 700, H, True) for x in calls))
+    tok = torch.arange(700, dtype=torch.int32, device="cuda").repeat(2, 1)
+    keep, src, left = _i32([300, 250]), torch.zeros(nB, 700, dtype=torch.int32, device="cuda"), _i32([0, 0])
+    ev_ws, w_new, t_new = B.workspace(B.d3tom_cache_evict_workspace_bytes(c.handle, 700)), torch.zeros(nB, 700, device="cuda"), torch.zeros_like(tok)
+
+    def attend(x, o, w):
+        B.d3tom_attend_cache(x["q"], c.handle, x["off"], x["m"], 700, 0.1, False, o, ws, weight_out=w)
+
+    def evict(w):
+        B.d3tom_cache_evict(c.handle, 700, keep, 2, 9, w, tok, w_new, t_new, left, ev_ws, src=src)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for x in calls:
+            attend(x, x["o"], x["w"])
+    side.synchronize()
+    kept = [c.k_pages.clone(), c.v_pages.clone()]
+    graphs = []
+    for x in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            attend(x, x["o"], x["w"])
+    for i in range(4):
+        want = []
+        for x in calls:
+            x["q"].normal_()
+            want.append((torch.zeros_like(x["o"]), torch.zeros_like(x["w"])))
+            attend(x, *want[-1])
+        for x in calls:
+            x["o"].zero_()
+            x["w"].zero_()
+        for g in (graphs if i % 2 else graphs[::-1]):
+            g.replay()
+        torch.cuda.synchronize()
+        for x, (o, w) in zip(calls, want):
+            assert torch.equal(x["o"], o) and all(torch.equal(x["w"][b, :n], w[b, :n]) for b, n in enumerate(lens)), i
+    # the eviction, captured on its own workspace, by other weights at each replay
+    w = calls[0]["w"]
+    evict(w)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        evict(w)
+    for i in range(4):
+        w.uniform_()
+        c.k_pages.copy_(kept[0])
+        c.v_pages.copy_(kept[1])
+        graph.replay()
+        torch.cuda.synchronize()
+        for b, n in enumerate(lens):
+            assert np.array_equal(src[b, :int(left[b])].cpu().numpy(), OC.evict(w[b, :n].cpu().numpy(), np.arange(n), int(keep[b]), 2, 9)), i
+
+
+def test_two_streams_at_once(B):
+    # calls on streams, caches and workspaces of their own give what they give alone
+    jobs = []
+    for i, (m, lens) in enumerate([(1, [5000, 900]), (20, [1500, 2100])]):
+        c = Cache(B, lens, 2, 128, 64, "bf16", seed=20 + i)
+        q = torch.randn(2 * m, 8, 128, device="cuda").bfloat16()
+        n = max(lens)
+        job = dict(c=c, q=q, off=_i32([0, m, 2 * m]), m=m, n=n, keep=_i32([x // 2 for x in lens]), ws=B.workspace(B.d3tom_attend_cache_workspace_bytes(c.handle, 2 * m, m, n, 8, True)),
+                   ev=B.workspace(B.d3tom_cache_evict_workspace_bytes(c.handle, n)), tok=torch.arange(n, dtype=torch.int32, device="cuda").repeat(2, 1), pages=(c.k_pages.clone(), c.v_pages.clone()),
+                   stream=torch.cuda.Stream())
+        jobs.append(job)
+
+    def run(j, stream=None):
+        out = dict(o=torch.zeros_like(j["q"]), w=torch.zeros(2, j["n"], device="cuda"), w2=torch.zeros(2, j["n"], device="cuda"), t2=torch.zeros_like(j["tok"]),
+                   left=_i32([0, 0]), src=torch.zeros_like(j["tok"]))
+        torch.cuda.synchronize()
+        return out, lambda: (B.d3tom_attend_cache(j["q"], j["c"].handle, j["off"], j["m"], j["n"], 0.1, False, out["o"], j["ws"], weight_out=out["w"], stream=stream),
+                             B.d3tom_cache_evict(j["c"].handle, j["n"], j["keep"], 4, 16, out["w"], j["tok"], out["w2"], out["t2"], out["left"], j["ev"], src=out["src"], stream=stream))
+    alone, pages = [], []
+    for j in jobs:
+        out, call = run(j)
+        call()
+        torch.cuda.synchronize()
+        alone.append(out)
+        pages.append((j["c"].k_pages.clone(), j["c"].v_pages.clone()))
+    for _ in range(3):
+        for j in jobs:
+            j["c"].k_pages.copy_(j["pages"][0])
+            j["c"].v_pages.copy_(j["pages"][1])
+        both = [run(j, j["stream"]) for j in jobs]
+        for _, call in both:
+            call()
+        torch.cuda.synchronize()
+        for j, (out, _), want, page in zip(jobs, both, alone, pages):
+            assert all(torch.equal(out[t], want[t]) for t in ("o", "w", "w2", "t2", "left", "src"))
+            assert all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in zip((j["c"].k_pages, j["c"].v_pages), page))
 
 
 def test_streams_and_devices(B):
