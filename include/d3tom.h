@@ -533,11 +533,12 @@ int d3tom_cache_append(const d3tom_paged_cache* cache /* host */, const void* k,
  *   weight_in  float[B, weight_stride] or NULL (zeros); may be weight_out
  * bf16: the probabilities enter the product with v as bf16, relative to the running maximum of their row, all sums are float32.
  * Long caches are cut into runs of slots whose results are joined; how goes by the host-known sizes only, so that a call has
- * the same bits whatever the cache's unused slots hold.  Calls of more than 16 million workgroups
+ * the same bits whatever the cache's unused slots hold.  max_len above D3TOM_MAX_CACHE_LEN and calls of more than 16 million workgroups
  * (samples * max_q * H times the runs of a cache) return D3TOM_ERR_UNSUPPORTED.
  * Workspace: d3tom_attend_cache_workspace_bytes (weighed: whether weight_out is given; 0 for arguments that the call refuses), which is
  * enough for every call on the cache with at most these rows, max_len and H, weighed or not, whatever max_q.
  * ---------------------------------------------------------------------------------------- */
+#define D3TOM_MAX_CACHE_LEN 134217728
 size_t d3tom_attend_cache_workspace_bytes(const d3tom_paged_cache* cache /* host */, int rows, int max_q, int max_len, int H, int weighed);
 int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_paged_cache* cache /* host */, const int32_t* q_off, int rows, int max_q,
                        int max_len, int H, float scale, int causal, void* o, float* lse, const float* weight_in, float* weight_out,

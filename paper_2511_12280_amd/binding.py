@@ -35,7 +35,7 @@ D3TOM_MAX_VISUAL, D3TOM_MAX_DECIDERS = 16384, 256
 D3TOM_IMPORTANCE_STATIC_BYTES = 16 << 20
 D3TOM_AXES_SHARED, D3TOM_AXES_OWN = 0, 1
 D3TOM_MAX_AXES = 4
-D3TOM_MAX_EVICT_LEN = 1 << 20
+D3TOM_MAX_CACHE_LEN, D3TOM_MAX_EVICT_LEN = 1 << 27, 1 << 20
 D3TOM_LINEAR_PLAIN, D3TOM_LINEAR_RESIDUAL, D3TOM_LINEAR_SWIGLU, D3TOM_LINEAR_PARTIAL, D3TOM_LINEAR_ROPE = range(5)
 
 EXPORTS = ["d3tom_keep_count", "d3tom_schedule", "d3tom_model_flops", "d3tom_workspace_bytes",

@@ -1177,6 +1177,7 @@ static int attend_cache_check(const d3tom_paged_cache* c, int rows, int max_q, i
     if (rc != D3TOM_OK) return rc;
     if (rows < 1 || max_q < 1 || max_q > rows || max_len < 1 || H < 1 || H % c->Hkv) return D3TOM_ERR_INVALID_ARG;
     if ((int64_t)max_len > (int64_t)c->table_stride * c->page_size) return D3TOM_ERR_INVALID_ARG;
+    if (max_len > D3TOM_MAX_CACHE_LEN) return D3TOM_ERR_UNSUPPORTED;                // 512 threads for every 32 slots: fewer than 2^32
     return D3TOM_OK;
 }
 

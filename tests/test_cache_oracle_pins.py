@@ -181,6 +181,10 @@ def test_attend_cache_refuses(B):
         assert B._lib.d3tom_attend_cache_workspace_bytes(_cache(B), rows, most, max_len, H, 0) == 0
     assert _attend(lib, B, cache=_cache(B, B=65535), rows=1 << 30, most=1 << 30) == UNSUPPORTED
     assert _attend(lib, B, qs=(1 << 23) + 8) == UNSUPPORTED
+    endless = _cache(B, page_size=4096, table_stride=1 << 19)
+    for n in ((1 << 27) + 1, 2 ** 31 - 1):
+        assert _attend(lib, B, cache=endless, max_len=n, wo=P, stride=n) == UNSUPPORTED
+        assert B._lib.d3tom_attend_cache_workspace_bytes(endless, 5, 3, n, 4, 1) == 0
 
 
 def test_attend_cache_workspace_serves_smaller_calls(B):
