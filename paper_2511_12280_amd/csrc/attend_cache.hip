@@ -174,16 +174,27 @@ typedef __attribute__((__vector_size__(4 * sizeof(short)))) short ac_short4;
 typedef __attribute__((__vector_size__(8 * sizeof(short)))) short ac_short8;
 
 #if defined(__HIP_DEVICE_COMPILE__)
-template <typename T>
 __device__ __forceinline__ f32x4 ac_mma(const uint4& a, const uint4& b, f32x4 c) {
-    if constexpr (sizeof(T) == 2) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    } else {
-        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// Float32 logits as four sums side by side.  One after the other, dh / 4 roundings deep, they were most of the output's error where a sample has few slots: over 600
+// calls of all lengths, its ratio to the error of the same attention in elementary float32 operations was 1.08 in the middle and 3.6 at most, and is 0.63 and 1.5.  5 rows over
+// 213 slots 6.9 -> 6.5 us, a row each over 16 samples of 1000 slots (32 heads over 8 of 64) 18.1 -> 17.3; 32 rows each over 4 of 1500 (8 over 2 of 128) 20.9 -> 21.1.
+template <int KS>
+__device__ __forceinline__ f32x4 ac_logits_f32(const uint4 (&k)[KS], const uint4 (&q)[KS]) {
+    f32x4 sum[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
-        return c;
+    for (int e = 0; e < 4; ++e) sum[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+        const f32x4 x = __builtin_bit_cast(f32x4, k[kk]), y = __builtin_bit_cast(f32x4, q[kk]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], sum[e], 0, 0, 0);
     }
+    f32x4 all;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) all[e] = (sum[0][e] + sum[1][e]) + (sum[2][e] + sum[3][e]);
+    return all;
 }
 __device__ __forceinline__ float quad_max(float v) { return quad_combine(v, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float quad_sum(float v) { return quad_combine(v, [](float a, float b) { return a + b; }); }
@@ -351,9 +362,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
         f32x4 st[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-            st[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (sizeof(T) == 2) {
+                st[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int kk = 0; kk < KS; ++kk) st[kb] = ac_mma<T>(*reinterpret_cast<const uint4*>(w + k_addr[kk] + kb * 16 * ROWB), qf[kk], st[kb]);
+                for (int kk = 0; kk < KS; ++kk) st[kb] = ac_mma(*reinterpret_cast<const uint4*>(w + k_addr[kk] + kb * 16 * ROWB), qf[kk], st[kb]);
+            } else {
+                uint4 kf[KS];
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk) kf[kk] = *reinterpret_cast<const uint4*>(w + k_addr[kk] + kb * 16 * ROWB);
+                st[kb] = ac_logits_f32(kf, qf);
+            }
         }
         wait_lds();
         if (t + 2 < mine) issue_k(t + 2);
@@ -605,16 +623,23 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
         __builtin_amdgcn_sched_barrier(0);
     };
     auto scores = [&]() {                              // S = K Q^T
-#pragma unroll
-        for (int kb = 0; kb < KW; ++kb)
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) st[qb][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kk = 0; kk < KS; ++kk)
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int kb = 0; kb < KW; ++kb)
 #pragma unroll
-                for (int qb = 0; qb < QB; ++qb) st[qb][kb] = ac_mma<T>(kf[kb][kk], qf[qb][kk], st[qb][kb]);
+                for (int qb = 0; qb < QB; ++qb) st[qb][kb] = ac_logits_f32(kf[kb], qf[qb]);
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < KW; ++kb)
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) st[qb][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk)
+#pragma unroll
+                for (int kb = 0; kb < KW; ++kb)
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb) st[qb][kb] = ac_mma(kf[kb][kk], qf[qb][kk], st[qb][kb]);
+        }
         __builtin_amdgcn_sched_barrier(0);
     };
     auto softmax = [&](int t) {
@@ -959,12 +984,17 @@ __global__ __launch_bounds__(CW_WAVES * 64, 2) void cache_weigh_kernel(AttendCac
             if (seen_x >= a.G) { seen_x -= a.G; ++seen_i; }
             const bool masked = __builtin_amdgcn_ballot_w64(limit < key0 + KEYS) != 0;
             f32x4 st[KB];
+            if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) st[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int kb = 0; kb < KB; ++kb) st[kb] = ac_logits_f32(kf[kb], qf);
+            } else {
 #pragma unroll
-            for (int kk = 0; kk < KS; ++kk)
+                for (int kb = 0; kb < KB; ++kb) st[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int kb = 0; kb < KB; ++kb) st[kb] = ac_mma<T>(kf[kb][kk], qf[kk], st[kb]);
+                for (int kk = 0; kk < KS; ++kk)
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) st[kb] = ac_mma(kf[kb][kk], qf[kk], st[kb]);
+            }
             if (masked) {
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
