@@ -750,7 +750,8 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
 constexpr int JW_UNROLL = 4;
 __device__ __forceinline__ int runs_of(const AttendCacheArgs& a, int limit) { return max(1, (limit + a.run - 1) / a.run); }
 
-template <int NT> struct JoinLds { f32x4 t[NT]; float m[NT / 4], z[NT / 4]; };
+// (a group of threads may be a single one: float32 heads of 4 channels)
+template <int NT> struct JoinLds { f32x4 t[NT]; float m[NT], z[NT]; };
 template <typename T, int NT>
 __device__ __forceinline__ void join_rows(const AttendCacheArgs& a, int b, int block, int groups, JoinLds<NT>& lds) {
     const int tid = threadIdx.x, dh = a.cache.dh;
@@ -795,7 +796,7 @@ __device__ __forceinline__ void join_rows(const AttendCacheArgs& a, int b, int b
     }
     if (groups > 1) {
         lds.t[tid] = t;
-        if (c == 0 && y < NT / 4) { lds.m[y] = m; lds.z[y] = z; }
+        if (c == 0) { lds.m[y] = m; lds.z[y] = z; }
         __syncthreads();
         if (there && g == 0) {
             float mt = m;

@@ -313,6 +313,15 @@ def test_attend_cache_maximum_in_the_first_and_in_the_last_slot(B):
         _check_attend(_host(o), _host(lse), None, q, c.k[0], c.v[0], float(np.float32(0.1)), False, "bf16", None)
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,dh,lens,new,causal", [
+    ("bf16", 32, 8, 8, [2000], [2], False), ("f32", 32, 4, 4, [4000], [2], False), ("f32", 32, 8, 12, [2000], [2], True), ("f32", 16, 16, 8, [3000, 1301], [3, 2], True),
+    ("bf16", 32, 32, 8, [4096], [1], False), ("f32", 64, 1, 12, [5000, 40], [1, 1], True), ("bf16", 32, 2, 16, [2000], [2], True), ("f32", 32, 8, 20, [2000], [2], False)])
+@pytest.mark.parametrize("weighed", [False, True])
+def test_attend_cache_joins_runs_of_small_heads(B, dtype, H, Hkv, dh, lens, new, causal, weighed):
+    # more than four runs, which groups of threads share, and one to five threads to a group: up to 256 groups in a workgroup
+    _attend_case(B, dtype, H, Hkv, dh, 16, lens, new, causal, weighed)
+
+
 @pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 30), ("f32", 2)])
 def test_attend_cache_repeats_bit_by_bit_whatever_lies_behind(B, dtype, new):
     c, dq, o, lse, w, ws = _attend_case(B, dtype, 8, 2, 128, 16, [999, 130], [new, 1], True, True)
