@@ -37,9 +37,13 @@ __device__ __forceinline__ int sample_rows(const AttendCacheArgs& a, int b, int&
 // slots that row i of nq sees
 __device__ __forceinline__ int row_limit(const AttendCacheArgs& a, int n, int nq, int i) { return a.causal ? max(n - nq + i + 1, 0) : n; }
 
-template <typename T>
-__device__ __forceinline__ void store_out(T* p, const float* v, int n) {
-    for (int e = 0; e < n; ++e) Elem<T>::store(p + e, v[e]);
+// What a row's sum gives.  It is 0 where the row saw nothing (no slot, or logits of -infinity alone); NaN among its logits makes it NaN, which output, lse and weights then show.
+__device__ __forceinline__ float row_factor(float z) { return z == 0.f ? 0.f : 1.0f / z; }
+// (units of log 2; for the weights: whatever the logit of a row that saw nothing, 2^(logit - lse) is 0)
+__device__ __forceinline__ float weights_lse2(float m, float z) { return z == 0.f ? INFINITY : m + log2f(z); }
+__device__ __forceinline__ void store_lse(const AttendCacheArgs& a, size_t at, float m, float z) {
+    if (a.lse) a.lse[at] = (m + log2f(z)) * 0.6931471805599453f;
+    if (a.lse2) a.lse2[at] = weights_lse2(m, z);
 }
 
 // Any head size.  One workgroup per row, head and run: 256 slots at a time, 16 lanes to a key; for the output a thread takes one 16-byte chunk
@@ -133,15 +137,11 @@ __global__ __launch_bounds__(256) void attend_cache_generic_kernel(AttendCacheAr
         float t = 0.f;
         for (int x = 0; x < ngrp; ++x) t += sums[(x * nch + c) * EPC + e];
         if (a.S > 1) a.part_o[at * dh + tid] = t;
-        else Elem<T>::store(static_cast<T*>(a.o) + at * dh + tid, z > 0.f ? t / z : 0.f);
+        else Elem<T>::store(static_cast<T*>(a.o) + at * dh + tid, z == 0.f ? 0.f : t / z);
     }
     if (tid == 0) {
         if (a.S > 1) { a.part_ml[at * 2] = m; a.part_ml[at * 2 + 1] = z; }
-        else {
-            const float l2 = z > 0.f ? m + log2f(z) : -INFINITY;
-            if (a.lse) a.lse[at] = l2 * 0.6931471805599453f;
-            if (a.lse2) a.lse2[at] = l2;
-        }
+        else store_lse(a, at, m, z);
     }
 }
 
@@ -435,7 +435,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
         z += part_l[w][y] * f[w];
     }
     const size_t at = ((size_t)(r0 + yi) * a.H + yh) * a.S + s;
-    const float inv = a.S > 1 ? 1.f : z > 0.f ? 1.0f / z : 0.f;
+    const float inv = a.S > 1 ? 1.f : row_factor(z);
     const int c0 = (tid % TPR) * CH;
     float acc[CH];
 #pragma unroll
@@ -457,11 +457,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
 #pragma unroll
             for (int e = 0; e < CH; e += 4) *reinterpret_cast<f32x4*>(out + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
         }
-        if (c0 == 0) {
-            const float l2 = z > 0.f ? mt + log2f(z) : -INFINITY;
-            if (a.lse) a.lse[at] = l2 * 0.6931471805599453f;
-            if (a.lse2) a.lse2[at] = l2;
-        }
+        if (c0 == 0) store_lse(a, at, mt, z);
     }
 #endif
 }
@@ -721,7 +717,7 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
         // (in the same order in both waves)
         const float z = kg ? __builtin_fmaf(l2, f2, l[qb] * f1) : __builtin_fmaf(l[qb], f1, l2 * f2);
         const size_t at = (row[qb] * a.H + xh[qb]) * a.S + s;
-        const float inv = a.S > 1 ? 1.f : z > 0.f ? 1.0f / z : 0.f;
+        const float inv = a.S > 1 ? 1.f : row_factor(z);
 #pragma unroll
         for (int t = 0; t < HD; ++t) {
             const f32x4 x = kg ? o[qb][HD + t] : o[qb][t], y = swap[(((rg * QB + qb) * 2 + (kg ^ 1)) * HD + t) * 64 + lane];
@@ -735,11 +731,7 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
         }
         if (g == 0 && kg == 0) {
             if (a.S > 1) { a.part_ml[at * 2] = mt; a.part_ml[at * 2 + 1] = z; }
-            else {
-                const float lt = z > 0.f ? mt + log2f(z) : -INFINITY;
-                if (a.lse) a.lse[at] = lt * 0.6931471805599453f;
-                if (a.lse2) a.lse2[at] = lt;
-            }
+            else store_lse(a, at, mt, z);
         }
     }
 #endif
@@ -816,19 +808,15 @@ __device__ __forceinline__ void join_rows(const AttendCacheArgs& a, int b, int b
         }
     }
     if (!there || g != 0) return;
-    const float inv = z > 0.f ? 1.0f / z : 0.f;
+    const float inv = row_factor(z);
     T* o = static_cast<T*>(a.o) + at * dh + c * 4;
     const float w[4] = {t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv};
     if constexpr (sizeof(T) == 2) store_bf16<4>(o, w);
     else *reinterpret_cast<f32x4*>(o) = f32x4{w[0], w[1], w[2], w[3]};
-    if (c == 0) {
-        const float l2 = z > 0.f ? m + log2f(z) : -INFINITY;
-        if (a.lse) a.lse[at] = l2 * 0.6931471805599453f;
-        if (a.lse2) a.lse2[at] = l2;
-    }
+    if (c == 0) store_lse(a, at, m, z);
 }
 
-// log-sum-exp (units of log 2) of `cnt` rows and heads from item c0 on, into LDS: from their runs, by TPI threads to a row and head, or as it stands in a.lse2
+// log-sum-exp (weights_lse2) of `cnt` rows and heads from item c0 on, into LDS: from their runs, by TPI threads to a row and head, or as it stands in a.lse2
 template <int NT, int TPI>
 __device__ __forceinline__ void runs_lse2(const AttendCacheArgs& a, int r0, int nq, int n, int c0, int cnt, float* lse2) {
     constexpr int AT_ONCE = 8;                         // runs requested together
@@ -851,8 +839,12 @@ __device__ __forceinline__ void runs_lse2(const AttendCacheArgs& a, int r0, int 
             for (int i = 0; i < AT_ONCE; ++i) z += s + i * TPI < S ? v[i].y * __builtin_amdgcn_exp2f(v[i].x - ref) : 0.f;
         }
 #pragma unroll
-        for (int o = 1; o < TPI; o <<= 1) lse2_combine_fast(m, z, __shfl_xor(m, o), __shfl_xor(z, o));
-        if (sub == 0 && u < cnt) lse2[u] = m + log2f(z);
+        for (int o = 1; o < TPI; o <<= 1) {             // (a sum of NaN beside a maximum of -infinity stays NaN)
+            const float m2 = __shfl_xor(m, o), z2 = __shfl_xor(z, o), mn = fmaxf(m, m2), ref = mn == -INFINITY ? 0.f : mn;
+            z = z * __builtin_amdgcn_exp2f(m - ref) + z2 * __builtin_amdgcn_exp2f(m2 - ref);
+            m = mn;
+        }
+        if (sub == 0 && u < cnt) lse2[u] = weights_lse2(m, z);
     }
 }
 template <int NT>

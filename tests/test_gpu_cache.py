@@ -415,6 +415,63 @@ def test_attend_and_append_in_a_cache_above_four_gigabytes(B):
     assert torch.equal(kp[cache.page_table[0].long()[j // page], j % page], _dev(k[want], "bf16"))
 
 
+# ---- values that are not finite ----------------------------------------------------------------------------------------------------
+# (kernel and runs: waves of their own, one and many; shared tiles of 64 and 128 rows, one and many; any head size, one and many)
+NOT_FINITE = [("bf16", 8, 2, 128, [100, 37], [1, 2]), ("bf16", 8, 2, 64, [3000, 700], [2, 1]), ("bf16", 8, 2, 128, [90, 33], [12, 5]), ("bf16", 8, 2, 128, [1500, 260], [33, 7]),
+              ("bf16", 4, 2, 96, [200, 60], [3, 2]), ("bf16", 4, 2, 80, [2500, 60], [2, 1]), ("f32", 4, 2, 64, [100, 37], [5, 2]), ("f32", 8, 2, 128, [2100, 37], [3, 1]),
+              ("f32", 8, 2, 64, [300, 290], [40, 11]), ("f32", 4, 2, 40, [600, 70], [2, 1])]
+
+
+def _attend_call(B, c, q, new, causal, scale=0.1):
+    """outputs of one call on a cache whose pages hold c.k and c.v, and the weights that went in"""
+    nB, n, dev = len(c.lens), max(c.lens), dict(device="cuda")
+    for pages, rows in ((c.k_pages, c.k), (c.v_pages, c.v)):
+        for b, m in enumerate(c.lens):
+            j = np.arange(m)
+            pages[_i32(c.table[b, j // c.page]).long(), torch.arange(m, device="cuda") % c.page] = _dev(rows[b], c.dtype)
+    o, lse = torch.full(q.shape, 7.0, dtype=DT[c.dtype], **dev), torch.full(q.shape[:2], 7.0, **dev)
+    w_in, w_out = np.random.default_rng(3).random((nB, n)).astype(np.float32), torch.full((nB, n), -3.0, **dev)
+    ws = torch.full((B.d3tom_attend_cache_workspace_bytes(c.handle, len(q), max(new), n, q.shape[1], True),), 0xFF, dtype=torch.uint8, **dev)
+    B.d3tom_attend_cache(_dev(q, c.dtype), c.handle, _i32(_off(new)), max(new), n, scale, causal, o, ws, lse=lse, weight_in=_dev(w_in, "f32"), weight_out=w_out)
+    return _host(o), _host(lse), _host(w_out), w_in
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh,lens,new", NOT_FINITE)
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_attend_cache_a_row_of_nan_is_no_empty_row(B, dtype, H, Hkv, dh, lens, new, value):
+    # a key of NaN (or one of infinity, which makes NaN of its own row) in one head of the first sample: its heads give NaN, everywhere, and nothing else does
+    c = Cache(B, lens, Hkv, dh, 16, dtype, seed=[41, dh])
+    q = np.abs(_round(np.random.default_rng(6).standard_normal((sum(new), H, dh)), dtype))
+    c.k[0][lens[0] // 3, 0, 5] = value
+    o, lse, w, w_in = _attend_call(B, c, q, new, False)
+    m, G, s = new[0], H // Hkv, float(np.float32(0.1))
+    assert np.isnan(o[:m, :G]).all() and np.isnan(lse[:m, :G]).all() and np.isnan(w[0, :lens[0]]).all()
+    _check_attend(o[:m, G:], lse[:m, G:], None, q[:m, G:], c.k[0][:, 1:], c.v[0][:, 1:], s, False, dtype, None)
+    _check_attend(o[m:], lse[m:], w[1], q[m:], c.k[1], c.v[1], s, False, dtype, w_in[1])
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh,lens,new", NOT_FINITE)
+def test_attend_cache_logits_of_minus_infinity(B, dtype, H, Hkv, dh, lens, new):
+    # keys of one head of the first sample that no query looks at: zeros, lse -infinity, no weight.  Of the second one only the first key is seen.
+    c = Cache(B, lens, Hkv, dh, 16, dtype, seed=[42, dh])
+    q = np.abs(_round(np.random.default_rng(7).standard_normal((sum(new), H, dh)), dtype)) + 0.5
+    q = _round(q, dtype)
+    c.k[0][:, 0, 5] = -np.inf
+    c.k[1][1:, :, dh - 1] = -np.inf
+    o, lse, w, w_in = _attend_call(B, c, q, new, False)
+    m, G, s = new[0], H // Hkv, float(np.float32(0.1))
+    assert not o[:m, :G].any() and np.isneginf(lse[:m, :G]).all()
+    _check_attend(o[:m, G:], lse[:m, G:], None, q[:m, G:], c.k[0][:, 1:], c.v[0][:, 1:], s, False, dtype, None)
+    _check_attend(o[m:], lse[m:], None, q[m:], c.k[1][:1], c.v[1][:1], s, False, dtype, None)
+    got = OC.attend(q[:m, G:], c.k[0][:, 1:], c.v[0][:, 1:], s, False)[2] * (H - G) / H
+    E = s * max((np.abs(c.k[0][:, h // G]) @ np.abs(q[:m, h]).T).max() for h in range(G, H)) * (dh + 4) * U
+    big = s * max(np.abs(c.k[0][:, h // G] @ q[:m, h].T).max() for h in range(G, H))
+    d = np.expm1(4 * E + 8 * U * big) + (lens[0] + 64) * U
+    total = w_in[0, :lens[0]] + got
+    assert (np.abs(w[0, :lens[0]] - total) <= (d + (m * H + 8) * U) * got + 2 * U * total).all()
+    assert w[1, 0] == pytest.approx(w_in[1, 0] + new[1], rel=1e-5) and np.array_equal(w[1, 1:lens[1]].astype(np.float32), w_in[1, 1:lens[1]])
+
+
 # ---- eviction ----------------------------------------------------------------------------------------------------------------------
 def _evict_case(B, dtype, Hkv, dh, page, lens, keep, first, recent, seed=0, levels=0, aliased=False, odd=0, weights=None):
     c = Cache(B, lens, Hkv, dh, page, dtype, seed=[seed, len(lens), page])
