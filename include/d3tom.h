@@ -523,8 +523,8 @@ int d3tom_cache_append(const d3tom_paged_cache* cache /* host */, const void* k,
  * drafted ones, or the block of response positions that is being denoised).  Per row and head h, keys and values of head
  * h / (H / Hkv):  o = softmax(scale * q k^T) v over the sample's live slots, or, causal, over those up to the row's own slot
  * (row i of n: slot kv_len[b] - n + i).  A row that sees no slot gets zeros and lse -infinity, and so does one all of whose logits are
- * -infinity; NaN among a row's logits makes its o and lse, and the weights of the slots that it sees, NaN.  What lies behind a sample's last
- * slot is never used, NaN included.
+ * -infinity; NaN among a row's logits makes its o and lse, and the weights of the slots that it sees, NaN.  Slots that a
+ * row does not see, behind its own in the causal form or behind the sample's last one, have no part in its results, NaN and infinities included.
  *
  *   q          [rows, H, dh] dt, q_stride elements between rows (a multiple of 16 bytes, at most 16 MB); H a multiple of Hkv
  *   q_off      int32[B + 1]  first row of each sample; rows = q_off[B] (host-known), max_q the longest run, max_len the longest cache

@@ -244,8 +244,59 @@ __device__ __forceinline__ void ac_softmax(f32x4 (&st)[KB], f32x4 (&o)[DB], floa
 #endif
 }
 
+// The matrix instructions multiply values that a column does not see by its probability of 0, which NaN and infinities survive.  In tiles that not all columns see (of causal rows
+// alone, one or two of a run) such values of those slots are taken for 0, and where there were any, the columns that do see them get them behind the last tile: 0 + v is
+// what p v makes of a value that is not finite.  (Kernels of their own for such rows: others would be up to 1 % slower.  The looking itself: 32 rows each of 4 samples, 32 heads over 8 of
+// 128, bf16, and 2048 rows as before; 5 rows over 213 slots of float32 heads of 64 6.34 -> 6.48 us; 4 rows each of 8 samples of 1500 slots, bf16, 128 and 64 channels, 13.9 -> 14.1 and
+// 11.35 -> 11.56; 32 rows each of 2 of 1500, float32, 29.9 -> 30.8.)
+// A word of values of keys k0 and, bf16, k1 (its upper half): those that are not finite and not among the first `seen` keys to 0.
+template <typename T>
+__device__ __forceinline__ bool ac_clean(uint32_t& w, int k0, int k1, int seen) {
+    const uint32_t before = w;
+    if constexpr (sizeof(T) == 2) {
+        if (k0 >= seen && (w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
+        if (k1 >= seen && (w & 0x7F800000u) == 0x7F800000u) w &= 0xFFFFu;
+    } else {
+        if (k0 >= seen && (w & 0x7F800000u) == 0x7F800000u) w = 0u;
+    }
+    return w != before;
+}
+// the larger magnitudes of two words, as unsigned numbers; whether one of them belongs to a value that is not finite
+template <typename T>
+__device__ __forceinline__ uint32_t ac_magnitudes(uint32_t most, uint32_t w) {
+    if constexpr (sizeof(T) == 2) {
+        typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, most), __builtin_bit_cast(us2, w & 0x7FFF7FFFu)));
+    } else {
+        return max(most, w & 0x7FFFFFFFu);
+    }
+}
+template <typename T>
+__device__ __forceinline__ bool ac_not_finite(uint32_t most) { return most >= 0x7F800000u || (sizeof(T) == 2 && (most & 0xFFFFu) >= 0x7F80u); }
+// The values of one head in slots [from, to) that are not finite, to the columns that see them.  `mine(slot)`: whether the slot was in a tile of this wave.
+template <typename T, int DH, int QB, int DB, typename F>
+__device__ __forceinline__ void ac_add_not_finite(const AttendCacheArgs& a, int b, int kvh, int from, int to, F&& mine, f32x4 (&o)[QB][DB], const int (&limit)[QB]) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma nounroll
+    for (int j = from; j < to; ++j) {
+        if (!mine(j)) continue;
+        const T* v = static_cast<const T*>(a.v_pages) + a.cache.row(a.cache.readable(a.cache.page_of(b, j)), j) * a.cache.row_elems() + (size_t)kvh * DH + 4 * g;
+#pragma unroll
+        for (int t = 0; t < DB; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = Elem<T>::load(v + t * 16 + e);
+                const bool odd = (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u;
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb)
+                    if (odd && j < limit[qb]) o[qb][t][e] += x;
+            }
+    }
+}
+
+// UNEVEN: rows of a sample may see different numbers of slots.
 constexpr int WAVES = 4;
-template <typename T, int DH>
+template <typename T, int DH, bool UNEVEN>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCacheArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = AcTile<T, DH>;
@@ -340,10 +391,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
             v_addr[t] = C::TILE + 4 * g * ROWB + (((t * 4 + (r >> 2)) ^ C::v_turn(4 * g)) << 4) + (r & 3) * 4;
         }
     }
-    f32x4 o[DB];
+    f32x4 os[1][DB], (&o)[DB] = os[0];
 #pragma unroll
     for (int t = 0; t < DB; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
+    const int clean_from = limit0 < j1 ? limit0 : INT_MAX;     // (ac_clean)
+    bool cleaned = false;
     if (mine > 1) wait_loads<4 * C::LD>();             // the queries are there
     else if (mine > 0) wait_loads<2 * C::LD>();
     else wait_loads<0>();
@@ -384,6 +437,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
         if (t + 2 < mine) wait_loads<3 * C::LD>();         // V of this tile
         else if (t + 1 < mine) wait_loads<2 * C::LD>();
         else wait_loads<0>();
+        if (UNEVEN && key0 + KEYS > clean_from) {
+#pragma nounroll
+            for (int c = max(clean_from - key0, 0) * NCHK + lane; c < min(j1 - key0, KEYS) * NCHK; c += 64) {
+                uint4* chunk = reinterpret_cast<uint4*>(ring + wave * C::WAVE_LDS + (t & 1) * C::STAGE + C::TILE + c * 16);
+                uint32_t x[4] = {chunk->x, chunk->y, chunk->z, chunk->w};
+                bool changed = false;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) changed |= ac_clean<T>(x[i], 0, 0, 0);
+                if (changed) *chunk = make_uint4(x[0], x[1], x[2], x[3]);
+                cleaned |= changed;
+            }
+        }
         if constexpr (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) ac_short4* tr_ptr;
 #pragma unroll
@@ -410,6 +475,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
         }
         wait_lds();
         if (t + 2 < mine) issue_v(t + 2);
+    }
+    if (UNEVEN && __builtin_amdgcn_ballot_w64(cleaned) != 0) {
+        const int limits[1] = {limit};
+        ac_add_not_finite<T, DH>(a, b, kvh, max(limit0, j0), j1, [&](int j) { return ((j - j0) / KEYS) % WAVES == wave; }, os, limits);
     }
     wait_loads_and_barrier<0>();                           // nothing is on its way into the rings any more
     // the waves' parts, rows of queries
@@ -472,7 +541,7 @@ template <typename T, int DH> struct AcShared {
     static constexpr int KW = KB / 2;                  // blocks of 16 keys of a wave
     static constexpr int PAGES = 256;                  // blocks of 16 slots of a run whose pages lie in LDS
 };
-template <typename T, int DH, int QB>
+template <typename T, int DH, int QB, bool UNEVEN>
 __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = AcTile<T, DH>;
@@ -618,6 +687,31 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
             }
         __builtin_amdgcn_sched_barrier(0);
     };
+    const int clean_from = limit0 < j1 ? limit0 : INT_MAX;
+    bool cleaned = false;
+    auto clean_v = [&](int t) {                        // (see above; in registers: the tile is other rows' too)
+        const int seen = clean_from - (j0 + t * KEYS + kg * KW * 16);
+        if (seen >= KW * 16) return;
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < VN; ++i)
+#pragma unroll
+            for (int t2 = 0; t2 < DB; ++t2)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = ac_magnitudes<T>(most, __float_as_uint(vf[i][t2][e]));
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(ac_not_finite<T>(most)) == 0, 1)) return;
+#pragma unroll
+        for (int i = 0; i < VN; ++i)
+#pragma unroll
+            for (int t2 = 0; t2 < DB; ++t2)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t x = __float_as_uint(vf[i][t2][e]);
+                    const int at = sizeof(T) == 2 ? i * 32 + (e >> 1) * 16 + 4 * g + (e & 1) * 2 : i * 16 + 4 * g + e;
+                    cleaned |= ac_clean<T>(x, at, at + 1, seen);
+                    vf[i][t2][e] = __uint_as_float(x);
+                }
+    };
     auto scores = [&]() {                              // S = K Q^T
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -690,9 +784,12 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
         if (works) {
             read_v(t);
             softmax(t);
+            if (UNEVEN) clean_v(t);
             values();
         }
     }
+    if (UNEVEN && __builtin_amdgcn_ballot_w64(cleaned) != 0)
+        ac_add_not_finite<T, DH>(a, b, kvh, max(limit0, j0), j1, [&](int j) { return (((j - j0) % KEYS) / (KW * 16)) == kg; }, o, limit);
     wait_loads_and_barrier<0>();                       // nothing is on its way into LDS any more, and nobody reads the ring
     // wave kg keeps the channels of half kg and gives the others away
     f32x4* swap = reinterpret_cast<f32x4*>(ring);
@@ -1164,20 +1261,20 @@ static size_t attend_cache_ws_bytes(const d3tom_paged_cache& c, int rows, int ma
     const size_t plan = attend_cache_plan(c, rows, max_q, max_len, H, weighed).bytes;          // more only where max_q is not the longest run
     return bytes > plan ? bytes : plan;
 }
-template <typename T, int DH>
+template <typename T, int DH, bool UNEVEN>
 static int attend_cache_launch(const AttendCacheArgs& a, int kernel, hipStream_t st) {
     static PerDeviceOnce once;
     using C = AcTile<T, DH>;
     constexpr int WAVES_LDS = WAVES * C::WAVE_LDS + 16 * C::ROWB, ROWS_LDS = AcShared<T, DH>::LDS;
     constexpr int WIDE = C::KS > 4 ? 1 : 2;     // (float32 heads of 128 have no registers for 128 rows: the plan gives them 64)
     if (!once.run([] {
-            return raise_dynamic_lds(attend_cache_kernel<T, DH>, WAVES_LDS) && raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 1>, ROWS_LDS) &&
-                   raise_dynamic_lds(attend_cache_rows_kernel<T, DH, WIDE>, ROWS_LDS);
+            return raise_dynamic_lds(attend_cache_kernel<T, DH, UNEVEN>, WAVES_LDS) && raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 1, UNEVEN>, ROWS_LDS) &&
+                   raise_dynamic_lds(attend_cache_rows_kernel<T, DH, WIDE, UNEVEN>, ROWS_LDS);
         })) return D3TOM_ERR_DEVICE;
     const int wgs = (a.nB * a.cache.Hkv * a.S + 7) / 8 * 8 * a.tiles;
-    if (kernel == AC_WAVES) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH><<<wgs, 64 * WAVES, WAVES_LDS, st>>>(a)));
-    else if (kernel == AC_ROWS64) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, 1><<<wgs, 512, ROWS_LDS, st>>>(a)));
-    else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, WIDE><<<wgs, 512, ROWS_LDS, st>>>(a)));
+    if (kernel == AC_WAVES) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, UNEVEN><<<wgs, 64 * WAVES, WAVES_LDS, st>>>(a)));
+    else if (kernel == AC_ROWS64) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, 1, UNEVEN><<<wgs, 512, ROWS_LDS, st>>>(a)));
+    else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, WIDE, UNEVEN><<<wgs, 512, ROWS_LDS, st>>>(a)));
     return D3TOM_OK;
 }
 // threads that share a row's runs when `threads` join rows of dh channels
@@ -1241,8 +1338,11 @@ extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_p
     a.weight_in = weight_in; a.weight_out = weight_out; a.weight_stride = weight_stride;
     const bool bf16 = dt == D3TOM_BF16;
     if (p.kernel != AC_GENERIC) {
-        rc = bf16 ? (dh == 128 ? attend_cache_launch<uint16_t, 128>(a, p.kernel, st) : attend_cache_launch<uint16_t, 64>(a, p.kernel, st))
-                  : (dh == 128 ? attend_cache_launch<float, 128>(a, p.kernel, st) : attend_cache_launch<float, 64>(a, p.kernel, st));
+        const bool uneven = causal && max_q > 1;
+        if (bf16) rc = dh == 128 ? (uneven ? attend_cache_launch<uint16_t, 128, true>(a, p.kernel, st) : attend_cache_launch<uint16_t, 128, false>(a, p.kernel, st))
+                                 : (uneven ? attend_cache_launch<uint16_t, 64, true>(a, p.kernel, st) : attend_cache_launch<uint16_t, 64, false>(a, p.kernel, st));
+        else rc = dh == 128 ? (uneven ? attend_cache_launch<float, 128, true>(a, p.kernel, st) : attend_cache_launch<float, 128, false>(a, p.kernel, st))
+                            : (uneven ? attend_cache_launch<float, 64, true>(a, p.kernel, st) : attend_cache_launch<float, 64, false>(a, p.kernel, st));
         if (rc != D3TOM_OK) return rc;
     } else {
         const int wgs = cache->B * max_q * H * p.S;

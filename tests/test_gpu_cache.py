@@ -472,6 +472,32 @@ def test_attend_cache_logits_of_minus_infinity(B, dtype, H, Hkv, dh, lens, new):
     assert w[1, 0] == pytest.approx(w_in[1, 0] + new[1], rel=1e-5) and np.array_equal(w[1, 1:lens[1]].astype(np.float32), w_in[1, 1:lens[1]])
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,dh,lens,new", NOT_FINITE)
+@pytest.mark.parametrize("value,into", [(float("nan"), "v"), (float("inf"), "v"), (float("nan"), "k"), (-float("inf"), "kv")])
+def test_attend_cache_rows_in_front_do_not_see_what_is_not_finite(B, dtype, H, Hkv, dh, lens, new, value, into):
+    # causal, and some of the last slots, which later rows wrote, are not finite in one head: the rows in front of them, the other heads and the other sample are what they
+    # would be without them
+    c = Cache(B, lens, Hkv, dh, 16, dtype, seed=[43, dh])
+    q = _round(np.random.default_rng(8).standard_normal((sum(new), H, dh)), dtype)
+    n, m, G, s = lens[0], new[0], H // Hkv, float(np.float32(0.1))
+    first = (m + 1) // 2                                          # the first row that sees any of them
+    bad = n - m + first
+    if first < m:
+        for rows in [dict(k=c.k, v=c.v)[t] for t in into]:
+            rows[0][bad, 1], rows[0][n - 1, 1, dh - 3] = value, value
+    o, lse, w, w_in = _attend_call(B, c, q, new, True)
+    front, rest = slice(0, n - m + first), slice(first, m)
+    _check_attend(o[:first], lse[:first], None, q[:first], c.k[0][front], c.v[0][front], s, True, dtype, None)
+    _check_attend(o[m:], lse[m:], w[1], q[m:], c.k[1], c.v[1], s, True, dtype, w_in[1])
+    others = [h for h in range(H) if h // G != 1]
+    keys = [g for g in range(Hkv) if g != 1]
+    _check_attend(o[:m, others], lse[:m, others], None, q[:m, others], c.k[0][:, keys], c.v[0][:, keys], s, True, dtype, None)
+    if first < m and "v" in into:
+        assert not np.isfinite(o[rest, G:2 * G]).all()
+    if into == "v":
+        assert np.isfinite(lse).all() and np.isfinite(w[0, :n]).all()          # the probabilities are what they were
+
+
 # ---- eviction ----------------------------------------------------------------------------------------------------------------------
 def _evict_case(B, dtype, Hkv, dh, page, lens, keep, first, recent, seed=0, levels=0, aliased=False, odd=0, weights=None):
     c = Cache(B, lens, Hkv, dh, page, dtype, seed=[seed, len(lens), page])
