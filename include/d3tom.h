@@ -461,7 +461,8 @@ int d3tom_stack_step_batch(const void* x, int B, const int32_t* N /* host */, in
  * share pages that are only read.
  *
  *   k_pages, v_pages  [num_pages, page_size, Hkv, dh] dt
- *   page_table        int32[B, table_stride]; entries behind a sample's last page are never read
+ *   page_table        int32[B, table_stride], all of it readable memory; entries behind a sample's last page may be read (page numbers are
+ *                     requested together with the lengths), but whatever they hold has no part in any result
  *   kv_len            int32[B]  live slots of each sample.  The caller advances it BEFORE the rows are written: a call that appends
  *                     or attends from n new rows has them in slots kv_len - n .. kv_len - 1, and can be repeated.
  *   page_size         a power of two, 16 .. 4096          dh  a multiple of 8 (bf16) or 4 (f32), at most 256
@@ -537,7 +538,8 @@ int d3tom_cache_append(const d3tom_paged_cache* cache /* host */, const void* k,
  * the same bits whatever the cache's unused slots hold.  max_len above D3TOM_MAX_CACHE_LEN and calls of more than 16 million workgroups
  * (samples * max_q * H times the runs of a cache) return D3TOM_ERR_UNSUPPORTED.
  * Workspace: d3tom_attend_cache_workspace_bytes (weighed: whether weight_out is given; 0 for arguments that the call refuses), which is
- * enough for every call on the cache with at most these rows, max_len and H, weighed or not, whatever max_q.
+ * enough for every call on the cache with at most these rows, max_len and H, whatever max_q, if it gives no more than B * max_q rows; asked
+ * for with weights, it is enough for calls without them too (asked for without, not for calls with them).
  * ---------------------------------------------------------------------------------------- */
 #define D3TOM_MAX_CACHE_LEN 134217728
 size_t d3tom_attend_cache_workspace_bytes(const d3tom_paged_cache* cache /* host */, int rows, int max_q, int max_len, int H, int weighed);

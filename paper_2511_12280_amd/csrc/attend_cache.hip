@@ -1258,7 +1258,7 @@ static size_t attend_cache_ws_bytes(const d3tom_paged_cache& c, int rows, int ma
     const size_t parts = most < some ? most : some, kept = rh < (size_t)c.B * c.Hkv * 16 ? rh : (size_t)c.B * c.Hkv * 16;
     size_t bytes = 4 * 256 + parts * (c.dh * 4 + 8);
     if (weighed) bytes += rh * 4 + kept * ((max_len + 15) / 16 * 16) * 4;
-    const size_t plan = attend_cache_plan(c, rows, max_q, max_len, H, weighed).bytes;          // more only where max_q is not the longest run
+    const size_t plan = attend_cache_plan(c, rows, max_q, max_len, H, weighed).bytes;          // more only for more rows than B * max_q
     return bytes > plan ? bytes : plan;
 }
 template <typename T, int DH, bool UNEVEN>
