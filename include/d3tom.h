@@ -535,8 +535,9 @@ int d3tom_cache_append(const d3tom_paged_cache* cache /* host */, const void* k,
  *   weight_in  float[B, weight_stride] or NULL (zeros); may be weight_out
  * bf16: the probabilities enter the product with v as bf16, relative to the running maximum of their row, all sums are float32.
  * Long caches are cut into runs of slots whose results are joined; how goes by the host-known sizes only, so that a call has
- * the same bits whatever the cache's unused slots hold.  max_len above D3TOM_MAX_CACHE_LEN and calls of more than 16 million workgroups
- * (samples * max_q * H times the runs of a cache) return D3TOM_ERR_UNSUPPORTED.
+ * the same bits whatever the cache's unused slots hold.  max_len above D3TOM_MAX_CACHE_LEN, samples * max_q * H above 16 million (heads other than
+ * 64 and 128: that times the runs of a cache) and more than 8 million workgroups (16 million where 16 rows at most share a key head) return
+ * D3TOM_ERR_UNSUPPORTED.
  * Workspace: d3tom_attend_cache_workspace_bytes (weighed: whether weight_out is given; 0 for arguments that the call refuses), which is
  * enough for every call on the cache with at most these rows, max_len and H, whatever max_q, if it gives no more than B * max_q rows; asked
  * for with weights, it is enough for calls without them too (asked for without, not for calls with them).

@@ -1261,6 +1261,12 @@ static size_t attend_cache_ws_bytes(const d3tom_paged_cache& c, int rows, int ma
     const size_t plan = attend_cache_plan(c, rows, max_q, max_len, H, weighed).bytes;          // more only for more rows than B * max_q
     return bytes > plan ? bytes : plan;
 }
+// What the launches of a plan hold: workgroups of the attention (512 threads where rows share tiles), and the rows and heads that the joining goes over, which also bound a row's number.
+static bool attend_cache_fits(const d3tom_paged_cache& c, const AttendCachePlan& p, int max_q, int H) {
+    const double items = (double)c.B * max_q * H;
+    const double groups = p.kernel == AC_GENERIC ? items * p.S : (double)c.B * c.Hkv * p.S * p.tiles;
+    return items <= CACHE_MOST_GROUPS && groups <= (p.kernel == AC_GENERIC || p.kernel == AC_WAVES ? CACHE_MOST_GROUPS : CACHE_MOST_GROUPS / 2);
+}
 template <typename T, int DH, bool UNEVEN>
 static int attend_cache_launch(const AttendCacheArgs& a, int kernel, hipStream_t st) {
     static PerDeviceOnce once;
@@ -1322,7 +1328,7 @@ extern "C" int d3tom_attend_cache(const void* q, int64_t q_stride, const d3tom_p
     if (!q_off || !ws || !(scale > 0.f) || !(scale < 3.0e38f)) return D3TOM_ERR_INVALID_ARG;
     if ((weight_in && !weight_out) || (weight_out && weight_stride < max_len)) return D3TOM_ERR_INVALID_ARG;
     const AttendCachePlan p = attend_cache_plan(*cache, rows, max_q, max_len, H, weight_out != nullptr);
-    if ((double)cache->B * max_q * H * p.S > CACHE_MOST_GROUPS || (double)max_q * H > CACHE_MOST_GROUPS) return D3TOM_ERR_UNSUPPORTED;
+    if (!attend_cache_fits(*cache, p, max_q, H)) return D3TOM_ERR_UNSUPPORTED;
     if (ws_bytes < attend_cache_ws_bytes(*cache, rows, max_q, max_len, H, weight_out != nullptr) || (((uintptr_t)ws) & 255u)) return D3TOM_ERR_WORKSPACE_TOO_SMALL;
     AttendCacheArgs a{};
     a.cache = cache_view(*cache);

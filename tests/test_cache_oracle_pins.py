@@ -187,6 +187,16 @@ def test_attend_cache_refuses(B):
         assert B._lib.d3tom_attend_cache_workspace_bytes(endless, 5, 3, n, 4, 1) == 0
 
 
+def test_attend_cache_refuses_launches_that_are_too_large(B):
+    lib = _lib(B)
+    far = dict(page_size=4096, table_stride=1 << 12)
+    for kw in (dict(cache=_cache(B, **far), rows=1 << 22, most=1 << 22),                                                     # rows and heads
+               dict(cache=_cache(B, B=65535, **far), rows=17, most=17, H=2, max_len=62 * 4096),                               # workgroups of 512 threads
+               dict(cache=_cache(B, B=65535, **far), rows=1, most=1, H=2, max_len=123 * 4096),                                # of 256
+               dict(cache=_cache(B, B=65535, dh=96, **far), rows=200, most=200, H=2, qs=256)):                                # of any head size
+        assert _attend(lib, B, **kw) == UNSUPPORTED, kw
+
+
 def test_attend_cache_workspace_serves_smaller_calls(B):
     import random
     rng = random.Random(0)

@@ -285,6 +285,12 @@ def test_attend_cache_padded_rows_and_generous_maxima(B, dtype, H, Hkv, dh, new,
     _attend_case(B, dtype, H, Hkv, dh, 16, [200, 131], new, True, weighed, pad=13, more_q=more_q, more_len=17)
 
 
+@pytest.mark.parametrize("weighed", [False, True])
+def test_attend_cache_maxima_far_above_what_there_is(B, weighed):
+    # samples * max_q * H * runs is beyond 2^24, the workgroups are 2^17
+    _attend_case(B, "bf16", 8, 2, 64, 64, [16384] + [20, 300] * 31 + [5], [1] * 63 + [3], True, weighed, pad=8192, more_q=8189)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("std,scale", [(30.0, None), (1.0, 1e-6), (1.0, 4.0)])
 def test_attend_cache_logits_far_apart_and_all_alike(B, dtype, std, scale):
