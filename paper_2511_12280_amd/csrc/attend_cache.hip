@@ -23,7 +23,7 @@ struct AttendCacheArgs {
     float *part_o, *part_ml;                    // [rows, H, S, dh], [rows, H, S, 2]
     float* logits;                              // [rows, H, lpad], units of log 2, or none
     int last_slot;                              // that a sample's part of the page table has a place for
-    int lpad, tiles;                            // tiles: of 16 rows, of a sample and key head
+    int lpad, tiles;                            // tiles: of 64 or 128 rows, of a sample and key head
     const float* weight_in;
     float* weight_out;
     int weight_stride;
@@ -304,34 +304,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
     extern __shared__ __attribute__((aligned(16))) char ring[];
     __shared__ float part_m[WAVES][16], part_l[WAVES][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-    // Tiles of rows of the same keys run on one XCD, one after the other; first runs first, so that the XCDs (every eighth workgroup) have samples
-    // of all lengths, and first runs, which every sample has, do not meet on some of them.
-    int id = blockIdx.x;
-    const int xcd = id & 7;
-    id >>= 3;
-    int tile = 0;
-    if (a.tiles > 1) { tile = id % a.tiles; id /= a.tiles; }
-    int unit = id * 8 + xcd;
+    // First runs first, so that the XCDs (every eighth workgroup) have samples of all lengths, and first runs, which every sample has, do not meet on some of them.
+    int unit = blockIdx.x;
     const int heads = a.nB * a.cache.Hkv, s = __builtin_amdgcn_readfirstlane(div_by(unit, heads, a.per_heads));
     unit -= s * heads;
     const int b = __builtin_amdgcn_readfirstlane(div_by(unit, a.cache.Hkv, a.per_Hkv)), kvh = unit - b * a.cache.Hkv;
-    if (s >= a.S) return;
     // Pages of this wave's blocks of 16 slots: lane i has that of block i % KB of its tile i / KB.  Requested with the sample's sizes, not behind them: what lies
     // behind its last page is never used.
     const int j0 = s * a.run, my_slot = j0 + ((lane / KB) * WAVES + wave) * KEYS + (lane % KB) * 16;
     const int my_page = a.cache.page_of(b, min(my_slot, a.last_slot));
     int r0;
     const int nq = sample_rows(a, b, r0);
-    const int R = nq * a.G, R0 = tile * 16;
-    if (R0 >= R) return;
+    const int R = nq * a.G;                            // 16 at most
+    if (R <= 0) return;
     const int n = a.cache.length(b, a.max_len);
-    const int last = min(R0 + 15, R - 1);
-    const int j1 = min(row_limit(a, n, nq, div_by(last, a.G, a.per_G)), j0 + a.run);
+    const int j1 = min(row_limit(a, n, nq, nq - 1), j0 + a.run);
     if (j0 >= j1 && s > 0) return;
-    const int x = min(R0 + r, R - 1), xi = div_by(x, a.G, a.per_G), xh = kvh * a.G + (x - xi * a.G);          // this lane's column
+    const int x = min(r, R - 1), xi = div_by(x, a.G, a.per_G), xh = kvh * a.G + (x - xi * a.G);          // this lane's column
     const size_t row = (size_t)(r0 + xi);
     const int limit = min(row_limit(a, n, nq, xi), j1);
-    const int limit0 = min(row_limit(a, n, nq, div_by(R0, a.G, a.per_G)), j1);                                 // slots that all columns see
+    const int limit0 = min(row_limit(a, n, nq, 0), j1);                                                        // slots that all columns see
 
     const int ntile = j1 > j0 ? (j1 - j0 + KEYS - 1) / KEYS : 0;
     const int mine = (ntile - wave + WAVES - 1) / WAVES;                                       // tiles wave, wave + WAVES, ...
@@ -367,13 +359,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
     // bytes of a row at a time, they are slower than the keys, and these waited for them: 1 us.)
     const uint32_t q_lds = (uint32_t)(size_t)(lds_ptr_t)ring + WAVES * C::WAVE_LDS;
     constexpr int QLD = 16 / RPI;
-    const __amdgpu_buffer_rsrc_t rq = make_uniform_rsrc(static_cast<const char*>(a.q) + ((size_t)(r0 + div_by(R0, a.G, a.per_G)) * a.q_stride + (size_t)kvh * a.G * DH) * sizeof(T), ~0u);
+    const __amdgpu_buffer_rsrc_t rq = make_uniform_rsrc(static_cast<const char*>(a.q) + ((size_t)r0 * a.q_stride + (size_t)kvh * a.G * DH) * sizeof(T), ~0u);
 #pragma unroll
     for (int i = 0; i < (QLD + WAVES - 1) / WAVES; ++i) {
         const int li = i * WAVES + wave;
         if (QLD % WAVES == 0 || li < QLD) {
-            const int x2 = li * RPI + ld_row, X = min(R0 + x2, R - 1), Xi = div_by(X, a.G, a.per_G);
-            direct_load_16(rq, (uint32_t)((Xi - div_by(R0, a.G, a.per_G)) * (int)a.q_stride + (X - Xi * a.G) * DH) * sizeof(T) + ((ld_pos ^ C::k_turn(x2)) << 4), q_lds + li * 1024);
+            const int x2 = li * RPI + ld_row, X = min(x2, R - 1), Xi = div_by(X, a.G, a.per_G);
+            direct_load_16(rq, (uint32_t)(Xi * (int)a.q_stride + (X - Xi * a.G) * DH) * sizeof(T) + ((ld_pos ^ C::k_turn(x2)) << 4), q_lds + li * 1024);
         }
     }
     if (mine > 0) { issue_k(0); issue_v(0); }
@@ -405,7 +397,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) qf[kk] = *reinterpret_cast<const uint4*>(ring + WAVES * C::WAVE_LDS + k_addr[kk]);
     float* kept = a.logits ? a.logits + (row * a.H + xh) * a.lpad : nullptr;
-    const bool real = R0 + r < R;
+    const bool real = r < R;
 
     for (int t = 0; t < mine; ++t) {
         const char* w = ring + wave * C::WAVE_LDS + (t & 1) * C::STAGE;
@@ -491,9 +483,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
     __syncthreads();
     // four threads of every wave to a row
     constexpr int TPR = 4 * WAVES, CH = DH / TPR;
-    const int y = tid / TPR, Y = R0 + y;
-    if (Y >= R) return;
-    const int yi = div_by(Y, a.G, a.per_G), yh = kvh * a.G + (Y - yi * a.G);
+    const int y = tid / TPR;
+    if (y >= R) return;
+    const int yi = div_by(y, a.G, a.per_G), yh = kvh * a.G + (y - yi * a.G);
     float mt = -INFINITY;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) mt = fmaxf(mt, part_m[w][y]);
@@ -552,6 +544,7 @@ __global__ __launch_bounds__(512, 2) void attend_cache_rows_kernel(AttendCacheAr
     __shared__ float other_m[2][4][QB * 16], other_l[2][4][QB * 16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     const int kg = wave >> 2, rg = wave & 3;
+    // Tiles of rows of the same keys run on one XCD, one after the other; first runs first (see above).
     int id = blockIdx.x;
     const int xcd = id & 7;
     id >>= 3;
@@ -1277,8 +1270,8 @@ static int attend_cache_launch(const AttendCacheArgs& a, int kernel, hipStream_t
             return raise_dynamic_lds(attend_cache_kernel<T, DH, UNEVEN>, WAVES_LDS) && raise_dynamic_lds(attend_cache_rows_kernel<T, DH, 1, UNEVEN>, ROWS_LDS) &&
                    raise_dynamic_lds(attend_cache_rows_kernel<T, DH, WIDE, UNEVEN>, ROWS_LDS);
         })) return D3TOM_ERR_DEVICE;
-    const int wgs = (a.nB * a.cache.Hkv * a.S + 7) / 8 * 8 * a.tiles;
-    if (kernel == AC_WAVES) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, UNEVEN><<<wgs, 64 * WAVES, WAVES_LDS, st>>>(a)));
+    const int units = a.nB * a.cache.Hkv * a.S, wgs = (units + 7) / 8 * 8 * a.tiles;
+    if (kernel == AC_WAVES) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_kernel<T, DH, UNEVEN><<<units, 64 * WAVES, WAVES_LDS, st>>>(a)));
     else if (kernel == AC_ROWS64) D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, 1, UNEVEN><<<wgs, 512, ROWS_LDS, st>>>(a)));
     else D3TOM_LAUNCH(CACHE_ATTEND, st, (attend_cache_rows_kernel<T, DH, WIDE, UNEVEN><<<wgs, 512, ROWS_LDS, st>>>(a)));
     return D3TOM_OK;
