@@ -285,6 +285,22 @@ def test_attend_cache_padded_rows_and_generous_maxima(B, dtype, H, Hkv, dh, new,
     _attend_case(B, dtype, H, Hkv, dh, 16, [200, 131], new, True, weighed, pad=13, more_q=more_q, more_len=17)
 
 
+@pytest.mark.parametrize("H,Hkv,dh,lens,new,causal", [(8, 2, 128, [37, 5], [1, 1], False), (32, 32, 128, [300, 65], [1, 1], False), (8, 2, 64, [90, 40], [4, 2], True), (16, 1, 64, [4000], [1], False),
+                                                      (4, 2, 128, [2500, 333], [3, 8], True), (4, 4, 64, [30, 17], [16, 2], False)])
+def test_attend_cache_few_rows_do_not_round_probabilities(B, H, Hkv, dh, lens, new, causal):
+    # probabilities enter the product with v in two bf16 parts: the upper bits leave less than 2^-7 of one, of which rounding takes 2^-8 at most: 2^-15 instead of the 2^-8 of one part
+    c, dq, o, lse, _, _ = _attend_case(B, "bf16", H, Hkv, dh, 16, lens, new, causal, False, seed=12)
+    q, G, scale, off = _host(dq), H // Hkv, float(np.float32(1.0 / np.sqrt(dh))), _off(new)
+    for b in range(len(lens)):
+        r, k, v, n = slice(off[b], off[b + 1]), c.k[b], c.v[b], lens[b]
+        want = OC.attend(q[r], k, v, scale, causal)[0]
+        E = max(scale * (np.abs(k[:, h // G]) @ np.abs(q[r, h]).T).max() for h in range(H)) * (dh + 4) * U
+        big = scale * max(np.abs(k[:, h // G] @ q[r, h].T).max() for h in range(H))
+        d = np.expm1(4 * E + 8 * U * big) + (n + 64) * U
+        spread = np.stack([OC.attend(q[r, h:h + 1], k[:, h // G:h // G + 1], np.abs(v[:, h // G:h // G + 1]), scale, causal)[0][:, 0] for h in range(H)], 1)
+        assert (np.abs(_host(o[r]) - want) <= (d + 2.0 ** -15) * spread * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want)).all()
+
+
 @pytest.mark.parametrize("weighed", [False, True])
 def test_attend_cache_maxima_far_above_what_there_is(B, weighed):
     # samples * max_q * H * runs is beyond 2^24, the workgroups are 2^17
