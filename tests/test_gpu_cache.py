@@ -437,6 +437,64 @@ def test_attend_and_append_in_a_cache_above_four_gigabytes(B):
     assert torch.equal(kp[cache.page_table[0].long()[j // page], j % page], _dev(k[want], "bf16"))
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,dh,new,n,weighed", [("bf16", 2, 1, 64, 1, (1 << 27) - 4101, False), ("bf16", 4, 1, 128, 5, (1 << 25) + 77, False), ("f32", 2, 2, 64, 1, 1 << 25, False),
+                                                          ("bf16", 1, 1, 80, 1, (1 << 22) - 3, False), ("bf16", 2, 1, 64, 1, (1 << 23) + 9, True), ("f32", 20, 1, 64, 1, (1 << 22) + 1, True)])
+def test_attend_cache_of_the_largest_lengths(B, dtype, H, Hkv, dh, new, n, weighed):
+    # one sample whose pages are the same few again and again: the attention over those, each key as often as its page comes
+    # Float32 sums: no lane adds up more than the 4096 slots of a run, no thread of the joining more than 2048 runs, with a few additions between lanes and threads
+    page, few = 4096, 2
+    rng = np.random.default_rng([n, dh])
+    k, v = (_round(rng.standard_normal((few * page, Hkv, dh)), dtype) for _ in range(2))
+    q = _round(rng.standard_normal((new, H, dh)), dtype)
+    entries = -(-n // page)
+    table = torch.arange(entries, dtype=torch.int32, device="cuda").remainder(few)[None].contiguous()
+    cache = B.PagedCache(_dev(k.reshape(few, page, Hkv, dh), dtype), _dev(v.reshape(few, page, Hkv, dh), dtype), table, _i32([n]))
+    o, lse = torch.zeros(new, H, dh, dtype=DT[dtype], device="cuda"), torch.zeros(new, H, device="cuda")
+    w = torch.full((1, n), -3.0, device="cuda") if weighed else None
+    B.d3tom_attend_cache(_dev(q, dtype), cache, _i32([0, new]), new, n, 0.3, False, o, B.workspace(B.d3tom_attend_cache_workspace_bytes(cache, new, new, n, H, weighed)), lse=lse, weight_out=w)
+    slots = np.arange(few * page)
+    often = (n - slots + few * page - 1) // (few * page)                          # how often each key comes
+    scale, G = float(np.float32(0.3)), H // Hkv
+    E = max(scale * (np.abs(k[:, h // G]) @ np.abs(q[:, h]).T).max() for h in range(H)) * (dh + 4) * U
+    big = scale * max(np.abs(k[:, h // G] @ q[:, h].T).max() for h in range(H))
+    d = np.expm1(4 * E + 8 * U * (big + np.log(n))) + (4096 + 2048 + 64) * U
+    b, half = 2.0 ** -8 if dtype == "bf16" else U, 2.0 ** -8 if dtype == "bf16" else 0.0
+    got, total = _host(o), np.zeros(few * page)
+    for i in range(new):
+        for h in range(H):
+            x = scale * (k[:, h // G] @ q[i, h])
+            p = often * np.exp(x - x.max())
+            want_lse = x.max() + np.log(p.sum())
+            p /= p.sum()
+            want, spread = p @ v[:, h // G], p @ np.abs(v[:, h // G])
+            assert (np.abs(got[i, h] - want) <= (d + half) * spread + b * np.abs(want) * (1 + b)).all(), (i, h, np.abs(got[i, h] - want).max())
+            assert abs(float(lse[i, h]) - want_lse) <= 2 * E + d + 4 * U * (abs(want_lse) + big)
+            total += p / often / H
+    if weighed:
+        want_w = torch.from_numpy(total).cuda().repeat(-(-n // (few * page)))[:n]
+        assert float(((w[0].double() - want_w).abs() / want_w).max()) <= (d + (new * H + 8) * U) * 1.01
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,new", [("bf16", 8, 8, [16, 1]), ("bf16", 8, 2, [40, 9]), ("f32", 4, 1, [70, 3]), ("bf16", 8, 1, [33, 128])])
+def test_attend_cache_rows_far_apart(B, dtype, H, Hkv, new):
+    # 16 MB between the rows of q, the most there may be: offsets of up to 2^31 bytes inside a tile
+    for dh in (64, 128, 96):
+        c = Cache(B, [300, 140], Hkv, dh, 16, dtype, seed=[51, dh])
+        rows, n = sum(new), 300
+        stride = (16 << 20) // (2 if dtype == "bf16" else 4)
+        wide = torch.empty(rows, stride, dtype=DT[dtype], device="cuda")
+        q = torch.randn(rows, H, dh, device="cuda").to(DT[dtype])
+        far = wide[:, stride - H * dh:].view(rows, H, dh)
+        far.copy_(q)
+        ws = B.workspace(B.d3tom_attend_cache_workspace_bytes(c.handle, rows, max(new), n, H, True))
+        outs = []
+        for x in (q, far):
+            o, lse, w = torch.zeros_like(q), torch.zeros(rows, H, device="cuda"), torch.zeros(2, n, device="cuda")
+            B.d3tom_attend_cache(x, c.handle, _i32(_off(new)), max(new), n, 0.1, True, o, ws, lse=lse, weight_out=w)
+            outs.append((o, lse, w))
+        assert all(torch.equal(a, b) for a, b in zip(*outs)) and torch.isfinite(outs[0][0]).all() and outs[0][2].any()
+
+
 # ---- values that are not finite ----------------------------------------------------------------------------------------------------
 # (kernel and runs: waves of their own, one and many; shared tiles of 64 and 128 rows, one and many; any head size, one and many)
 NOT_FINITE = [("bf16", 8, 2, 128, [100, 37], [1, 2]), ("bf16", 8, 2, 64, [3000, 700], [2, 1]), ("bf16", 8, 2, 128, [90, 33], [12, 5]), ("bf16", 8, 2, 128, [1500, 260], [33, 7]),
@@ -591,6 +649,16 @@ def test_cache_evict_weights_close_together(B, n, cluster, ties):
     above = int((w > 3).sum())
     for keep in {above + 1, above + 2, above + cluster // 2, above + cluster - 1, above + cluster}:
         _evict_case(B, "bf16", 1, 8, 16, [n], [keep], 0, 0, weights=w[None])
+
+
+def test_cache_evict_of_the_largest_length(B):
+    # 2^20 slots, 256 slices; and a neighbour that has a few
+    _evict_case(B, "bf16", 1, 8, 4096, [1 << 20, 77], [(1 << 19) + 13, 50], 4, 5000)
+
+
+def test_cache_evict_of_large_rows(B):
+    # rows of 2 MB, 64 of a word's slots moved: their chunks do not fit 24 bits at once
+    _evict_case(B, "f32", 2048, 256, 16, [130], [64], 0, 0, weights=np.arange(130, dtype=np.float32)[None])
 
 
 def test_cache_evict_protects_by_number(B):
