@@ -1223,8 +1223,9 @@ __global__ __launch_bounds__(256) void cache_weigh_generic_kernel(AttendCacheArg
 // How a call goes: a rule on host-known sizes only.
 //   heads of 64 and 128   up to 16 rows to a key head: waves on their own; more: 64 or 128 rows that share tiles.  A run for every compute unit: more runs cost a round of
 //                         workgroups each (32 samples of 2048 slots, 8 key heads of 128 in one, two, four rounds 49, 54, 57 us), fewer leave units idle (8 samples 17.3
-//                         and 16.2 us with 128 and 256).  One run, without the joining, where a head's K is short: one sample, 8 heads of 128, 512, 768 and
-//                         1024 slots 7.2, 8.7 and 10.4 us against 9.9, 9.9 and 9.8 in runs of 256; float32 heads of 64, 256 and 512 slots 7.1 and 10.6 against 9.8 and 10.0.
+//                         and 16.2 us with 128 and 256).  One run, without the joining, where a head's K is short, at most 128 KB (bf16) or 96 KB: one sample,
+//                         8 heads of 128, 512 and 768 slots 7.3 and 9.1 us in one run, 8.1 and 7.9 in several; heads of 64, 1024 and 1280 slots 7.7 and 8.8, 8.2 and 8.2; float32 heads
+//                         of 128, 192 slots 8.7, 9.9; of 64, 384 and 512 slots 8.2 and 9.8, 8.0 and 8.1.  (4 samples: the same.)
 //   others                a workgroup per row, head and run
 enum { AC_GENERIC = 0, AC_WAVES, AC_ROWS64, AC_ROWS128 };
 struct AttendCachePlan {
@@ -1244,7 +1245,7 @@ static AttendCachePlan attend_cache_plan(const d3tom_paged_cache& c, int rows, i
     long long S = groups >= want[p.kernel] ? 1 : want[p.kernel] / groups;
     const long long most = (max_len + step - 1) / step;
     S = S > most ? most : S;
-    if (p.kernel == AC_WAVES && (size_t)max_len * c.dh * elem_bytes(c.dt) <= (c.dt == D3TOM_BF16 ? 192u : 96u) * 1024) S = 1;
+    if (p.kernel == AC_WAVES && (size_t)max_len * c.dh * elem_bytes(c.dt) <= (c.dt == D3TOM_BF16 ? 128u : 96u) * 1024) S = 1;
     p.run = (int)((most + S - 1) / S * step);
     if (p.kernel != AC_GENERIC && p.run > AC_MAX_RUN) p.run = AC_MAX_RUN;
     p.S = (max_len + p.run - 1) / p.run;
