@@ -441,34 +441,28 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
                 cleaned |= changed;
             }
         }
+        // Probabilities as two bf16 parts, their upper bits and what is left (2^-15 of them goes): rounded to one part they were a quarter of the output's error (relative to the
+        // same in 64 bits 2.2e-3, now 1.65e-3, the output's own rounding), and matrix instructions are not what bounds few rows: a row each of 16 samples of 900 .. 2688 slots
+        // (weighed) 36.8 -> 37.1 us, one of 3709 slots and 32 key heads 15.4 -> 15.6, of 8 samples of 400 slots 7.5 -> 7.8, of 512 slots and 8 key heads 6.9 -> 7.2, 4 rows each of 8 samples of 1500
+        // slots and 64 channels 11.3 -> 11.0.  (The second part's product behind the request of the tile after the next, its values in registers: in front of it 0 .. 0.1 us more.  The
+        // second parts in the place of columns that there are not: no faster.)
+        constexpr int PAIRS = sizeof(T) == 2 ? KB / 2 : 1;
+        bf16x8 v8[PAIRS][DB];
         if constexpr (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) ac_short4* tr_ptr;
 #pragma unroll
-            for (int kp = 0; kp < KB / 2; ++kp) {
-                // Probabilities as two bf16 parts, their upper bits and what is left (2^-15 of them goes): rounded to one part they were a quarter of the output's error (relative to the
-                // same in 64 bits 2.2e-3, now 1.65e-3, the output's own rounding), and matrix instructions are not what bounds few rows: a row each of 16 samples of 900 .. 2688 slots 36.9 -> 36.95 us,
-                // one of 3709 slots and 32 key heads 15.5 -> 15.7, of 8 samples of 400 slots 7.6 -> 7.9.
-                uint4 upper;
-                bf16x8 lower;
-                uint32_t* up = &upper.x;
+            for (int kp = 0; kp < PAIRS; ++kp) {
+                uint32_t upper[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p0 = st[2 * kp + i / 2][(i & 1) * 2], p1 = st[2 * kp + i / 2][(i & 1) * 2 + 1];
-                    up[i] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
-                    lower[2 * i] = (__bf16)(p0 - bf16_lo(up[i]));
-                    lower[2 * i + 1] = (__bf16)(p1 - bf16_hi(up[i]));
-                }
-                bf16x8 v8[DB];
+                for (int i = 0; i < 4; ++i)
+                    upper[i] = __builtin_amdgcn_perm(__float_as_uint(st[2 * kp + i / 2][(i & 1) * 2 + 1]), __float_as_uint(st[2 * kp + i / 2][(i & 1) * 2]), 0x07060302u);
 #pragma unroll
                 for (int t2 = 0; t2 < DB; ++t2) {
                     const char* p = w + v_addr[t2] + kp * 32 * ROWB;
                     const ac_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + 16 * ROWB));
-                    v8[t2] = __builtin_bit_cast(bf16x8, ac_short8(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)));
+                    v8[kp][t2] = __builtin_bit_cast(bf16x8, ac_short8(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)));
+                    o[t2] = ac_mma(__builtin_bit_cast(uint4, v8[kp][t2]), make_uint4(upper[0], upper[1], upper[2], upper[3]), o[t2]);
                 }
-#pragma unroll
-                for (int t2 = 0; t2 < DB; ++t2) o[t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8[t2], __builtin_bit_cast(bf16x8, upper), o[t2], 0, 0, 0);
-#pragma unroll
-                for (int t2 = 0; t2 < DB; ++t2) o[t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8[t2], lower, o[t2], 0, 0, 0);
             }
         } else {
 #pragma unroll
@@ -481,6 +475,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_cache_kernel(AttendCache
         }
         wait_lds();
         if (t + 2 < mine) issue_v(t + 2);
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int kp = 0; kp < PAIRS; ++kp) {
+                bf16x8 lower;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float p = st[2 * kp + e / 4][e % 4];
+                    lower[e] = (__bf16)(p - __uint_as_float(__float_as_uint(p) & 0xFFFF0000u));
+                }
+#pragma unroll
+                for (int t2 = 0; t2 < DB; ++t2) o[t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8[kp][t2], lower, o[t2], 0, 0, 0);
+            }
+        }
     }
     if (UNEVEN && __builtin_amdgcn_ballot_w64(cleaned) != 0) {
         const int limits[1] = {limit};
