@@ -533,6 +533,7 @@ int d3tom_cache_append(const d3tom_paged_cache* cache /* host */, const void* k,
  *   weight_out float[B, weight_stride] out or NULL: for every live slot weight_in plus the probabilities that the sample's rows give
  *              it, added over rows and averaged over heads (the importance map with all rows as deciders); other slots are left as they are
  *   weight_in  float[B, weight_stride] or NULL (zeros); may be weight_out
+ *   scale      finite and > 0
  * bf16, heads of 64 and 128: where more than 16 rows (max_q * H / Hkv) share a key head, the probabilities enter the product with v as bf16,
  * relative to the running maximum of their row; all sums are float32.
  * Long caches are cut into runs of slots whose results are joined; how goes by the host-known sizes only, so that a call has
